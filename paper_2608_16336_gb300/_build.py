@@ -55,7 +55,7 @@ def build_tracegen(force: bool = False) -> str:
 
 def mtsim_sources() -> list[str]:
     return [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith((".cu", ".cuh"))] + [
-        os.path.join(INCLUDE, "mtsim.h")
+        os.path.join(INCLUDE, "mtsim.h"), os.path.join(INCLUDE, "mtsim_ops.h")
     ]
 
 

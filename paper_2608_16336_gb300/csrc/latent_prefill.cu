@@ -1,0 +1,406 @@
+// latent_prefill.cu -- causal attention of ragged requests with expanded keys
+// and values (mtsim_ops.h).
+#include "tensor.cuh"
+
+#include <cmath>
+
+namespace mtop {
+namespace {
+
+// One block computes 256 queries of one head of one request, as two tiles of
+// 128 rows, over tiles of 128 keys:
+//   S_t = Q_t K^T          (tensor core, 32-bit sums in tensor memory)
+//   P_t = exp2(S_t - m)    (four warps a tile, one thread a row)
+//   O_t += P_t V           (tensor core, P read from tensor memory)
+// The tensor core alternates between the tiles, so that one tile's
+// exponentials overlap the other's products.  K and V pass through a ring of
+// 16 KB slots (128 rows of 64 elements) filled by bulk copies.
+constexpr int kTile = 128;
+constexpr int kSlotBytes = kTile * 128;
+constexpr int kSlots = 8;
+constexpr int kSoftWarps = 8;
+constexpr int kThreads = (kSoftWarps + 4) * 32;  // + products, copies, and two that only make up the warpgroup
+// Registers a thread: 3 warpgroups launch with 168 (504 in all); the two of
+// weights take 224, which holds a row's 128 scores without spilling.
+constexpr int kSoftRegs = 224, kOtherRegs = 56;
+constexpr int kShared = 6 * kSlotBytes + kSlots * kSlotBytes + 256;
+// Tensor memory columns: S (and P over its first half) and O of each tile.
+constexpr int kColS = 0, kColO = 256, kCols = 512;
+
+struct Args {
+    const int32_t *q_offsets, *k_offsets;
+    void *out;
+    float *lse;
+    int64_t out_row, out_head;
+    int q_rows, k_rows;
+    int requests, heads, longest;
+    int head_blocks, key_blocks, value_blocks;  // of 64 elements
+    int value_dim;
+    int causal;
+    int group;       // heads that run side by side (their keys and values stay in L2)
+    int row_blocks;  // of 256 queries
+    float scale_log2;  // |scale| log2(e)
+    bool negative;
+};
+
+struct Barriers {
+    uint64_t q_full, full[kSlots], empty[kSlots], s_ready[2], p_ready[2], o_ready[2];
+    uint32_t tmem;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1)
+k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_q, const __grid_constant__ CUtensorMap m_qr,
+          const __grid_constant__ CUtensorMap m_k, const __grid_constant__ CUtensorMap m_kr,
+          const __grid_constant__ CUtensorMap m_v) {
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const uint32_t q_at = smem_addr(smem), ring = q_at + 6 * kSlotBytes;
+    Barriers *bars = (Barriers *)(smem + (6 + kSlots) * kSlotBytes);
+
+    // which rows: within a group of heads the last (longest) row blocks come first
+    int item = blockIdx.x;
+    const int per_request = a.row_blocks * a.heads;
+    const int b = item / per_request;
+    item -= b * per_request;
+    const int g0 = item / (a.row_blocks * a.group) * a.group, in_group = min(a.group, a.heads - g0);
+    item -= g0 * a.row_blocks;
+    const int h = g0 + item % in_group, row0 = (a.row_blocks - 1 - item / in_group) * 2 * kTile;
+    const int q0 = min(max(a.q_offsets[b], 0), a.q_rows), q1 = min(a.q_offsets[b + 1], a.q_rows);
+    const int k0 = min(max(a.k_offsets[b], 0), a.k_rows), k1 = min(a.k_offsets[b + 1], a.k_rows);
+    const int nq = q1 - q0, nk = max(k1 - k0, 0), rows = min(nq, a.longest);
+    if (row0 >= rows) return;
+    const int last0 = min(row0 + kTile, rows) - 1, last1 = min(row0 + 2 * kTile, rows) - 1;
+    const bool two = row0 + kTile < rows;
+    const int sees0 = a.causal ? min(nk, last0 + nk - nq + 1) : nk, sees1 = a.causal ? min(nk, last1 + nk - nq + 1) : nk;
+    const int n0 = sees0 > 0 ? (sees0 + kTile - 1) / kTile : 0, n1 = two && sees1 > 0 ? (sees1 + kTile - 1) / kTile : 0;
+    const int n = max(n0, n1);
+    const int qk_blocks = a.head_blocks + a.key_blocks;
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    bool dead = false;
+    if (threadIdx.x == 0) {
+        bar_init(smem_addr(&bars->q_full), 1);
+        for (int s = 0; s < kSlots; ++s) bar_init(smem_addr(&bars->full[s]), 1), bar_init(smem_addr(&bars->empty[s]), 1);
+        for (int t = 0; t < 2; ++t) {
+            bar_init(smem_addr(&bars->s_ready[t]), 1);
+            bar_init(smem_addr(&bars->p_ready[t]), kTile);
+            bar_init(smem_addr(&bars->o_ready[t]), 1);
+        }
+        bar_init_done();
+    }
+    if (warp == kSoftWarps) tmem_alloc(smem_addr(&bars->tmem), kCols);
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    const uint32_t tmem = bars->tmem;
+
+    if (warp >= kSoftWarps) {
+        registers_down<kOtherRegs>();
+        // ---------------------------------------------------------- copies
+        if (warp == kSoftWarps + 1 && lane == 0 && n > 0) {
+            const uint32_t qf = smem_addr(&bars->q_full);
+            bar_expect(qf, (two ? 2 : 1) * qk_blocks * kSlotBytes);
+            for (int t = 0; t < (two ? 2 : 1); ++t)
+                for (int c = 0; c < qk_blocks; ++c) {
+                    const uint32_t dst = q_at + (t * 3 + c) * kSlotBytes;
+                    const int r = q0 + row0 + t * kTile;
+                    if (c < a.head_blocks) copy_box_3d(dst, &m_q, 64 * c, h, r, qf);
+                    else copy_box_3d(dst, &m_qr, 64 * (c - a.head_blocks), h, r, qf);
+                }
+            int slot = 0;
+            uint32_t round = 0;
+            auto next = [&]() -> uint32_t {
+                bar_wait(smem_addr(&bars->empty[slot]), (round & 1) ^ 1, dead);
+                bar_expect(smem_addr(&bars->full[slot]), kSlotBytes);
+                return ring + slot * kSlotBytes;
+            };
+            auto took = [&]() {
+                if (++slot == kSlots) slot = 0, ++round;
+            };
+            for (int i = 0; i < n; ++i) {
+                const int r = k0 + i * kTile;
+                for (int c = 0; c < qk_blocks; ++c, took()) {
+                    const uint32_t dst = next();
+                    if (c < a.head_blocks) copy_box_3d(dst, &m_k, 64 * c, h, r, smem_addr(&bars->full[slot]));
+                    else copy_box_2d(dst, &m_kr, 64 * (c - a.head_blocks), r, smem_addr(&bars->full[slot]));
+                }
+                for (int c = 0; c < a.value_blocks; ++c, took()) {
+                    const uint32_t dst = next();
+                    copy_box_3d(dst, &m_v, 64 * c, h, r, smem_addr(&bars->full[slot]));
+                }
+            }
+        }
+        // -------------------------------------------------------- products
+        if (warp == kSoftWarps && n > 0) {
+            const bool bf = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value;
+            const uint32_t word_s = product_word(kTile, kTile, bf, false, a.negative);
+            const uint32_t word_o = product_word(kTile, 64 * a.value_blocks, bf, true, false);
+            const int per_tile = qk_blocks + a.value_blocks;
+            const bool leader = lane == 0;
+            auto slot_of = [&](int stream) { return stream % kSlots; };
+            auto wait_full = [&](int stream, int count) {
+                for (int c = 0; c < count; ++c)
+                    bar_wait(smem_addr(&bars->full[slot_of(stream + c)]), (uint32_t)((stream + c) / kSlots) & 1, dead);
+            };
+            auto release = [&](int stream, int count) {
+                for (int c = 0; c < count; ++c) product_commit(smem_addr(&bars->empty[slot_of(stream + c)]));
+            };
+            auto scores = [&](int t, int i) {  // S_t = Q_t K_i^T
+                const int stream = i * per_tile;
+                for (int c = 0; c < qk_blocks; ++c) {
+                    const uint32_t qa = q_at + (t * 3 + c) * kSlotBytes, ka = ring + slot_of(stream + c) * kSlotBytes;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        product_ss(tmem + kColS + t * kTile, operand(qa + 32 * k, 16, 1024), operand(ka + 32 * k, 16, 1024), word_s,
+                                   c + k > 0);
+                }
+                product_commit(smem_addr(&bars->s_ready[t]));
+                if (t == (i < n1 ? 1 : 0)) release(stream, qk_blocks);
+            };
+            auto weighted = [&](int t, int i) {  // O_t += P_t V_i
+                const int stream = i * per_tile + qk_blocks;
+                if (a.value_blocks == 2 && slot_of(stream) == kSlots - 1) {
+                    // the two halves of V are not neighbours in the ring: one product each
+                    const uint32_t word_h = product_word(kTile, 64, bf, true, false);
+                    for (int c = 0; c < 2; ++c) {
+                        const uint32_t va = ring + slot_of(stream + c) * kSlotBytes;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            product_ts(tmem + kColO + t * kTile + 64 * c, tmem + kColS + t * kTile + 8 * k,
+                                       operand(va + 2048 * k, kSlotBytes, 1024), word_h, i + k > 0);
+                    }
+                } else {
+                    const uint32_t va = ring + slot_of(stream) * kSlotBytes;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        product_ts(tmem + kColO + t * kTile, tmem + kColS + t * kTile + 8 * k, operand(va + 2048 * k, kSlotBytes, 1024),
+                                   word_o, i + k > 0);
+                }
+                if (t == (i < n1 ? 1 : 0)) release(stream, a.value_blocks);
+                if (i == (t ? n1 : n0) - 1) product_commit(smem_addr(&bars->o_ready[t]));
+            };
+            bar_wait(smem_addr(&bars->q_full), 0, dead);
+            wait_full(0, qk_blocks);
+            if (leader) {
+                if (n0 > 0) scores(0, 0);
+                if (n1 > 0) scores(1, 0);
+            }
+            __syncwarp();
+            for (int i = 0; i < n; ++i) {
+                const int stream = i * per_tile + qk_blocks;
+                wait_full(stream, a.value_blocks);
+                if ((i + 1) * kTile > nk) {
+                    // rows past the request's keys hold another's values: zeros, so that 0 * NaN cannot appear
+                    for (int c = 0; c < a.value_blocks; ++c) {
+                        uint4 *rows_at = (uint4 *)(smem + (6 + slot_of(stream + c)) * kSlotBytes + (nk - i * kTile) * 128);
+                        for (int e = lane; e < ((i + 1) * kTile - nk) * 8; e += 32) rows_at[e] = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async();
+                    __syncwarp();
+                }
+                for (int t = 0; t < 2; ++t) {
+                    const int nt = t ? n1 : n0;
+                    if (i >= nt) continue;
+                    bar_wait(smem_addr(&bars->p_ready[t]), (uint32_t)i & 1, dead);
+                    tmem_after_sync();
+                    if (leader) weighted(t, i);
+                    __syncwarp();
+                    if (i + 1 < nt) {
+                        wait_full((i + 1) * per_tile, qk_blocks);
+                        if (leader) scores(t, i + 1);
+                        __syncwarp();
+                    }
+                }
+            }
+        }
+    } else {
+        registers_up<kSoftRegs>();
+        // ------------------------------------------------- weights and sums
+        const int t = warp / 4, row = row0 + t * kTile + (warp % 4) * 32 + lane;
+        const int nt = t ? n1 : n0;
+        const int sees = a.causal ? min(nk, row + nk - nq + 1) : nk;  // keys [0, sees) of this row
+        const int first_sees = a.causal ? min(nk, row - lane + nk - nq + 1) : nk;  // of the warp's first row: the fewest
+        const uint32_t lanes = (uint32_t)(warp % 4) << 21;
+        const uint32_t s_at = tmem + kColS + t * kTile + lanes, o_at = tmem + kColO + t * kTile + lanes;
+        const float scale = a.scale_log2;
+        float top = -INFINITY, sum = 0.f;  // top: of the scaled scores, as far as P has been scaled by it
+        for (int i = 0; i < nt; ++i) {
+            bar_wait(smem_addr(&bars->s_ready[t]), (uint32_t)i & 1, dead);
+            tmem_after_sync();
+            uint32_t s[128];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, s + 32 * c);
+            tmem_wait_ld();
+            float *x = (float *)s;
+            if ((i + 1) * kTile > first_sees) {
+                const int v = sees - i * kTile;
+#pragma unroll
+                for (int c = 0; c < 128; ++c)
+                    if (c >= v) x[c] = -INFINITY;
+            }
+            float m0 = x[0], m1 = x[1], m2 = x[2], m3 = x[3];
+#pragma unroll
+            for (int c = 4; c < 128; c += 4) {
+                m0 = fmaxf(m0, x[c]), m1 = fmaxf(m1, x[c + 1]), m2 = fmaxf(m2, x[c + 2]), m3 = fmaxf(m3, x[c + 3]);
+            }
+            const float high = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;
+            // The sums are rescaled only when the maximum has grown by 2^8:
+            // until then weights up to 256 are as exact, and O stays where it is.
+            const bool grow = high > top + 8.f || (top == -INFINITY && high > -INFINITY);
+            if (__any_sync(~0u, grow)) {
+                const float keep = grow ? (top == -INFINITY ? 0.f : exp2_fast(top - high)) : 1.f;
+                if (grow) top = high;
+                sum *= keep;
+                if (i > 0) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (32 * c < 64 * a.value_blocks) {
+                            uint32_t o[32];
+                            tmem_ld32(o_at + 32 * c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+                            tmem_st32(o_at + 32 * c, o);
+                        }
+                    }
+                }
+            }
+            const float base = top == -INFINITY ? 0.f : -top;
+            float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+            uint32_t p[64];
+#pragma unroll
+            for (int c = 0; c < 128; c += 4) {
+                float e0, e1, e2, e3;
+                fma2(e0, e1, x[c], x[c + 1], scale, scale, base, base);
+                fma2(e2, e3, x[c + 2], x[c + 3], scale, scale, base, base);
+                e0 = exp2_fast(e0), e1 = exp2_fast(e1), e2 = exp2_fast(e2), e3 = exp2_fast(e3);
+                add2(s0, s1, e0, e1);
+                add2(s2, s3, e2, e3);
+                p[c / 2] = pack2<T>(e0, e1);
+                p[c / 2 + 1] = pack2<T>(e2, e3);
+            }
+            tmem_st32(s_at, p);
+            tmem_st32(s_at + 32, p + 32);
+            tmem_wait_st();
+            tmem_before_sync();
+            bar_arrive(smem_addr(&bars->p_ready[t]));
+            sum += (s0 + s1) + (s2 + s3);
+        }
+        if (row < rows && a.lse)
+            a.lse[(int64_t)(q0 + row) * a.heads + h] = sum > 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        T *out = (T *)a.out + (int64_t)(q0 + row) * a.out_row + h * a.out_head;
+        if (nt > 0) {
+            bar_wait(smem_addr(&bars->o_ready[t]), 0, dead);
+            tmem_after_sync();
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (32 * c < 64 * a.value_blocks) {
+                uint32_t o[32];
+                if (nt > 0) {
+                    tmem_ld32(o_at + 32 * c, o);
+                    tmem_wait_ld();
+                }
+                if (row < rows) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8)
+                        if (32 * c + e < a.value_dim) {
+                            uint4 w;
+                            auto val = [&](int j) { return sum > 0.f ? __uint_as_float(o[e + j]) * inv : 0.f; };
+                            w.x = pack2<T>(val(0), val(1)), w.y = pack2<T>(val(2), val(3));
+                            w.z = pack2<T>(val(4), val(5)), w.w = pack2<T>(val(6), val(7));
+                            *(uint4 *)(out + 32 * c + e) = w;
+                        }
+                }
+            }
+        }
+    }
+    tmem_before_sync();
+    __syncthreads();
+    if (warp == kSoftWarps) tmem_free(tmem, kCols);
+}
+
+template <typename T>
+int run(const sim_op_latent_prefill_t *a, const Args &k, const CUtensorMap *m, unsigned grid, cudaStream_t st) {
+    if (!allow_shared(k_prefill<T>, kShared)) return SIM_ERR_CUDA;
+    k_prefill<T><<<grid, kThreads, kShared, st>>>(k, m[0], m[1], m[2], m[3], m[4]);
+    return launched("sim_op_latent_prefill");
+}
+
+}  // namespace
+
+unsigned prefill_faults() {
+    unsigned n = 0;
+    return cudaMemcpyFromSymbol(&n, g_faults, sizeof n) == cudaSuccess ? n : ~0u;
+}
+
+}  // namespace mtop
+
+using namespace mtop;
+
+extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *stream) {
+    if (!a) return fail(SIM_ERR_ARG, "args is NULL");
+    if (a->type != SIM_OP_BF16 && a->type != SIM_OP_FP16) return fail(SIM_ERR_ARG, "element type %d: 16-bit types only", a->type);
+    if (a->requests < 0 || a->heads < 0 || a->longest < 0 || a->q_rows < 0 || a->k_rows < 0)
+        return fail(SIM_ERR_ARG, "sizes must not be negative");
+    if (a->head_dim < 8 || a->head_dim > SIM_OP_MAX_HEAD || a->head_dim % 8)
+        return fail(SIM_ERR_ARG, "head_dim must be a multiple of 8 in [8, %d]", SIM_OP_MAX_HEAD);
+    if (a->key_dim < 0 || a->key_dim > SIM_OP_MAX_KEY || a->key_dim % 8)
+        return fail(SIM_ERR_ARG, "key_dim must be a multiple of 8 in [0, %d]", SIM_OP_MAX_KEY);
+    if (a->value_dim < 8 || a->value_dim > SIM_OP_MAX_HEAD || a->value_dim % 8)
+        return fail(SIM_ERR_ARG, "value_dim must be a multiple of 8 in [8, %d]", SIM_OP_MAX_HEAD);
+    if (a->causal != 0 && a->causal != 1) return fail(SIM_ERR_ARG, "causal must be 0 or 1");
+    if (!std::isfinite(a->scale)) return fail(SIM_ERR_ARG, "scale must be finite");
+    if (a->requests == 0 || a->longest == 0 || a->heads == 0 || a->q_rows == 0) return SIM_OK;
+    if (a->q_rows > INT32_MAX - 65536 || a->k_rows > INT32_MAX - 65536 || a->heads > 65535 || a->requests > 65535)
+        return fail(SIM_ERR_ARG, "rows must be below 2^31 - 2^16, heads and requests at most 65535");
+    if (!a->q || !a->out || !a->q_offsets || !a->k_offsets || (a->k_rows && (!a->key || !a->value || (a->key_dim && !a->shared))))
+        return fail(SIM_ERR_ARG, "q, key, shared, value, the offsets and out must not be NULL");
+    if (!aligned16(a->q) || !aligned16(a->key) || (a->key_dim && (!aligned16(a->shared) || a->shared_row % 8)) ||
+        !aligned16(a->value) || !aligned16(a->out) || a->q_row % 8 || a->q_head % 8 || a->key_row % 8 || a->key_head % 8 ||
+        a->value_row % 8 || a->value_head % 8 || a->out_row % 8 || a->out_head % 8)
+        return fail(SIM_ERR_ARG, "tensors must be aligned to 16 bytes, with strides that are multiples of 8 elements");
+    const bool bf = a->type == SIM_OP_BF16;
+    Args k;
+    k.q_offsets = a->q_offsets, k.k_offsets = a->k_offsets, k.out = a->out, k.lse = a->lse;
+    k.out_row = a->out_row, k.out_head = a->out_head, k.q_rows = (int)a->q_rows, k.k_rows = (int)a->k_rows;
+    k.requests = a->requests, k.heads = a->heads, k.longest = a->longest;
+    k.head_blocks = (a->head_dim + 63) / 64, k.key_blocks = (a->key_dim + 63) / 64, k.value_blocks = (a->value_dim + 63) / 64;
+    k.value_dim = a->value_dim, k.causal = a->causal;
+    k.scale_log2 = std::fmax(std::fabs(a->scale) * 1.4426950408889634f, 1e-30f);  // not 0: a masked score is -infinity times it
+    k.negative = a->scale < 0;
+    const int64_t longest = a->longest < a->q_rows ? a->longest : a->q_rows;
+    k.row_blocks = (int)((longest + 2 * kTile - 1) / (2 * kTile));
+    // Heads side by side: as many as keep their keys and values within about a third of L2.
+    const int64_t head_bytes = a->k_rows * (a->head_dim + a->value_dim) * 2;
+    const int64_t fit = head_bytes > 0 ? (40 << 20) / head_bytes : a->heads;
+    k.group = (int)(fit < 1 ? 1 : fit > a->heads ? a->heads : fit);
+    const int64_t grid = (int64_t)a->requests * k.row_blocks * a->heads;
+    if (grid > INT32_MAX) return fail(SIM_ERR_ARG, "requests * heads * longest is too large");
+
+    CUtensorMap m[5];
+    auto map3 = [&](CUtensorMap *to, const void *base, int dim, int64_t rows, int64_t head, int64_t row) {
+        const uint64_t size[3] = {(uint64_t)dim, (uint64_t)a->heads, (uint64_t)(rows > 0 ? rows : 1)};
+        const int64_t stride[2] = {a->heads > 1 ? head : 8, rows > 1 ? row : 8};
+        const uint32_t box[3] = {64, 1, kTile};
+        return box_map(to, base, bf, 3, size, stride, box);
+    };
+    const char *q_key = (const char *)a->q + 2 * a->head_dim;
+    bool ok = map3(&m[0], a->q, a->head_dim, a->q_rows, a->q_head, a->q_row) &&
+              map3(&m[1], a->key_dim ? q_key : a->q, a->key_dim ? a->key_dim : 8, a->q_rows, a->q_head, a->q_row);
+    // without keys nothing is copied: any valid map does
+    const void *key = a->k_rows ? a->key : a->q, *value = a->k_rows ? a->value : a->q;
+    ok = ok && map3(&m[2], key, a->head_dim, a->k_rows, a->key_head, a->key_row) &&
+         map3(&m[4], value, a->value_dim, a->k_rows, a->value_head, a->value_row);
+    if (ok) {
+        const bool has = a->k_rows && a->key_dim;
+        const uint64_t size[2] = {has ? (uint64_t)a->key_dim : 8u, has ? (uint64_t)a->k_rows : 1u};
+        const int64_t stride[1] = {has && a->k_rows > 1 ? a->shared_row : 8};
+        const uint32_t box[2] = {64, kTile};
+        ok = box_map(&m[3], has ? a->shared : a->q, bf, 2, size, stride, box);
+    }
+    if (!ok) return SIM_ERR_CUDA;
+    const cudaStream_t st = (cudaStream_t)stream;
+    return bf ? run<__nv_bfloat16>(a, k, m, (unsigned)grid, st) : run<__half>(a, k, m, (unsigned)grid, st);
+}
