@@ -124,7 +124,8 @@ int sim_op_latent_append(const sim_op_latent_append_t *args, void *cuda_stream);
  * Scores, statistics and sums are in 32 bits; only the weights exp(s - max)
  * are rounded to the inputs' type, for their product with c (a tensor-core
  * operand; their sum is of the unrounded ones, so lse keeps 32 bits).  Types: 16-bit.  Alignment: pointers and strides of q and cache
- * are multiples of 16 bytes (8 elements), rank a multiple of 64, key_dim of 8.
+ * are multiples of 16 bytes (8 elements), rank a multiple of 64, key_dim of 8;
+ * cache_block is a multiple of cache_row (a cache that is one layer of several is).
  * workspace: sim_op_latent_decode_workspace() bytes for the same sizes,
  * 256-byte aligned, contents need not be set; not to be shared by calls that overlap. */
 typedef struct {

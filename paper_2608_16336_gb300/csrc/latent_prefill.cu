@@ -26,6 +26,7 @@ constexpr int kSoftRegs = 224, kOtherRegs = 56;
 constexpr int kShared = 6 * kSlotBytes + kSlots * kSlotBytes + 256;
 // Tensor memory columns: S (and P over its first half) and O of each tile.
 constexpr int kColS = 0, kColO = 256, kCols = 512;
+constexpr uint32_t kHigh = operand_high(1024);
 
 struct Args {
     const int32_t *q_offsets, *k_offsets;
@@ -136,7 +137,6 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             const uint32_t word_s = product_word(kTile, kTile, bf, false, a.negative);
             const uint32_t word_o = product_word(kTile, 64 * a.value_blocks, bf, true, false);
             const int per_tile = qk_blocks + a.value_blocks;
-            const bool leader = lane == 0;
             auto slot_of = [&](int stream) { return stream % kSlots; };
             auto wait_full = [&](int stream, int count) {
                 for (int c = 0; c < count; ++c)
@@ -148,11 +148,11 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             auto scores = [&](int t, int i) {  // S_t = Q_t K_i^T
                 const int stream = i * per_tile;
                 for (int c = 0; c < qk_blocks; ++c) {
-                    const uint32_t qa = q_at + (t * 3 + c) * kSlotBytes, ka = ring + slot_of(stream + c) * kSlotBytes;
+                    const uint32_t q_low = operand_low(q_at + (t * 3 + c) * kSlotBytes, 16),
+                                   k_low = operand_low(ring + slot_of(stream + c) * kSlotBytes, 16);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        product_ss(tmem + kColS + t * kTile, operand(qa + 32 * k, 16, 1024), operand(ka + 32 * k, 16, 1024), word_s,
-                                   c + k > 0);
+                        product_ss<kHigh, kHigh>(tmem + kColS + t * kTile, q_low + 2 * k, k_low + 2 * k, word_s, c + k > 0);
                 }
                 product_commit(smem_addr(&bars->s_ready[t]));
                 if (t == (i < n1 ? 1 : 0)) release(stream, qk_blocks);
@@ -163,25 +163,24 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
                     // the two halves of V are not neighbours in the ring: one product each
                     const uint32_t word_h = product_word(kTile, 64, bf, true, false);
                     for (int c = 0; c < 2; ++c) {
-                        const uint32_t va = ring + slot_of(stream + c) * kSlotBytes;
+                        const uint32_t v_low = operand_low(ring + slot_of(stream + c) * kSlotBytes, kSlotBytes);
 #pragma unroll
                         for (int k = 0; k < 8; ++k)
-                            product_ts(tmem + kColO + t * kTile + 64 * c, tmem + kColS + t * kTile + 8 * k,
-                                       operand(va + 2048 * k, kSlotBytes, 1024), word_h, i + k > 0);
+                            product_ts<kHigh>(tmem + kColO + t * kTile + 64 * c, tmem + kColS + t * kTile + 8 * k, v_low + 128 * k, word_h,
+                                              i + k > 0);
                     }
                 } else {
-                    const uint32_t va = ring + slot_of(stream) * kSlotBytes;
+                    const uint32_t v_low = operand_low(ring + slot_of(stream) * kSlotBytes, kSlotBytes);
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        product_ts(tmem + kColO + t * kTile, tmem + kColS + t * kTile + 8 * k, operand(va + 2048 * k, kSlotBytes, 1024),
-                                   word_o, i + k > 0);
+                        product_ts<kHigh>(tmem + kColO + t * kTile, tmem + kColS + t * kTile + 8 * k, v_low + 128 * k, word_o, i + k > 0);
                 }
                 if (t == (i < n1 ? 1 : 0)) release(stream, a.value_blocks);
                 if (i == (t ? n1 : n0) - 1) product_commit(smem_addr(&bars->o_ready[t]));
             };
             bar_wait(smem_addr(&bars->q_full), 0, dead);
             wait_full(0, qk_blocks);
-            if (leader) {
+            if (elect_one()) {
                 if (n0 > 0) scores(0, 0);
                 if (n1 > 0) scores(1, 0);
             }
@@ -203,11 +202,11 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
                     if (i >= nt) continue;
                     bar_wait(smem_addr(&bars->p_ready[t]), (uint32_t)i & 1, dead);
                     tmem_after_sync();
-                    if (leader) weighted(t, i);
+                    if (elect_one()) weighted(t, i);
                     __syncwarp();
                     if (i + 1 < nt) {
                         wait_full((i + 1) * per_tile, qk_blocks);
-                        if (leader) scores(t, i + 1);
+                        if (elect_one()) scores(t, i + 1);
                         __syncwarp();
                     }
                 }

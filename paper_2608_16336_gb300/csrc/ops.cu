@@ -60,13 +60,14 @@ bool box_map(CUtensorMap *map, const void *base, bool bf16, int dims, const uint
     return r == CUDA_SUCCESS;
 }
 
+unsigned decode_faults();
 unsigned prefill_faults();
 
 }  // namespace mtop
 
 extern "C" int sim_op_faults(void) {
-    const unsigned n = mtop::prefill_faults();
-    return n > 0x7FFFFFFFu ? mtop::fail(SIM_ERR_CUDA, "the fault counter cannot be read") : (int)n;
+    const unsigned d = mtop::decode_faults(), p = mtop::prefill_faults(), n = d + p;
+    return d == ~0u || p == ~0u || n > 0x7FFFFFFFu ? mtop::fail(SIM_ERR_CUDA, "the fault counter cannot be read") : (int)n;
 }
 
 extern "C" const char *sim_op_last_error(void) { return mtop::t_error; }

@@ -25,14 +25,23 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
 
 // Waits that ran out, counted per source file (sim_op_faults adds them up): a kernel
 // whose barrier never completes stops waiting after kWaitLimit tries
-// (seconds), counts here and ends.
+// (or kPollLimit polls: seconds), counts here and ends.
 static __device__ unsigned g_faults;
-constexpr int kWaitLimit = 1 << 22;
+constexpr int kWaitLimit = 1 << 22, kPollLimit = 1 << 26;
 
 __device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+
+// The same without waiting at all, for a thread that has other work.
+__device__ __forceinline__ bool bar_poll(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}"
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
@@ -60,6 +69,19 @@ __device__ __forceinline__ void copy_box_3d(uint32_t dst, const CUtensorMap *map
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
+// Four rows anywhere in a 2-d tensor, the map's box being one row high.
+__device__ __forceinline__ void copy_rows_4(uint32_t dst, const CUtensorMap *map, int x, int y0, int y1, int y2, int y3, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], "
+        "[%7];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y0), "r"(y1), "r"(y2), "r"(y3), "r"(bar)
+        : "memory");
+}
+// 16 bytes, or zeros where `real` is false.
+__device__ __forceinline__ void copy_16(uint32_t dst, const void *src, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_16_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // Generic writes to shared memory become visible to the tensor core and to bulk copies.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -98,15 +120,46 @@ __device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t *r) {
         : "memory");
 }
 
+// COLS columns of 16 lanes (the first or second half of the warp's 32), in the
+// register layout of a matrix fragment: registers 4k and 4k+1 of lane l are
+// columns 8k + 2 (l % 4) and the next of row l / 4, registers 4k+2 and 4k+3 of row l / 4 + 8.
+template <int COLS> __device__ __forceinline__ void tmem_ld_rows(uint32_t at, uint32_t *r);
+template <> __device__ __forceinline__ void tmem_ld_rows<32>(uint32_t at, uint32_t *r) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(at)
+                 : "memory");
+}
+template <> __device__ __forceinline__ void tmem_ld_rows<64>(uint32_t at, uint32_t *r) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(at)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st_rows64(uint32_t at, const uint32_t *r) {
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x8.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(at)
+                 : "memory");
+}
+
 // ---------------------------------------------------------- tensor core ---
 // A shared-memory operand in 128-byte-swizzled rows: 8 rows of 128 bytes make
 // a 1,024-byte atom.  With K along the rows (64 16-bit elements a row),
 // `stride` is the distance of 8-row groups along M or N, and a step of 16 along
 // K adds 32 bytes to the address.  With M or N along the rows, `stride`
 // is the distance of 8-row groups along K, and `lead` that of 64-element groups along M or N.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead, uint32_t stride) {
-    return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)((lead >> 4) & 0x3FFF) << 16 | (uint64_t)((stride >> 4) & 0x3FFF) << 32 |
-           (uint64_t)1 << 46 | (uint64_t)2 << 61;
+//
+// The low word holds the address (which steps, in units of 16 bytes) and
+// `lead`, the high word the rest, so that a step is one 32-bit addition.
+__device__ __forceinline__ uint32_t operand_low(uint32_t addr, uint32_t lead) { return (addr >> 4 & 0x3FFF) | lead >> 4 << 16; }
+__host__ __device__ constexpr uint32_t operand_high(uint32_t stride) { return stride >> 4 | 1u << 14 | 2u << 29; }
+
+// One thread of a converged warp.  The tensor core takes its operands from
+// registers that a warp has in common, and under this instruction's
+// predicate (unlike `lane == 0`) the compiler keeps them there.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p != 0;
 }
 
 // Instruction word of a product of 16-bit types into 32-bit sums.
@@ -115,17 +168,20 @@ __host__ __device__ constexpr uint32_t product_word(int m, int n, bool bf16, boo
            (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
 
-__device__ __forceinline__ void product_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t word, bool add) {
+template <uint32_t A_HIGH, uint32_t B_HIGH>
+__device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t word, bool add) {
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a),
-        "l"(b), "r"(word), "r"((uint32_t)add)
+        "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %6};\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d), "r"(a), "r"(b), "r"(word), "r"((uint32_t)add), "n"(A_HIGH),
+        "n"(B_HIGH)
         : "memory");
 }
 // A in tensor memory (two 16-bit elements a column).
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t word, bool add) {
+template <uint32_t B_HIGH>
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t word, bool add) {
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a),
-        "l"(b), "r"(word), "r"((uint32_t)add)
+        "{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.b32 p, %4, 0;\n mov.b64 b, {%2, %5};\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}" ::"r"(d), "r"(a), "r"(b), "r"(word), "r"((uint32_t)add), "n"(B_HIGH)
         : "memory");
 }
 // The barrier gets one arrival when every product this thread has queued is done.
