@@ -59,6 +59,8 @@ struct Args {
     int q_pad;                    // rows of Q kept: 16, 32 or 64
     int run;                      // tokens a copy takes
     bool scattered;               // four rows anywhere instead of a run
+    bool pair;                    // two row tiles of a part share their copies
+    bool q_flat;                  // Q's rows are one line to the copies
     int none;                     // a row outside the cache
     float scale_log2;
     bool negative;
@@ -105,7 +107,7 @@ struct Piece {
 };
 
 template <typename T, int TILE>
-__global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_cache) {
+__global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_cache, const __grid_constant__ CUtensorMap m_q) {
     using Z = Shape<TILE>;
     extern __shared__ __align__(1024) unsigned char smem[];
     // Q's column blocks hold only the rows there are (rounded up to 16, 32 or
@@ -122,14 +124,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
     asm volatile("griddepcontrol.launch_dependents;");
 
     if (warp == 0) {
-        // the line's length, and where this part begins on it
-        int total = 0;
-        for (int b0 = 0; b0 < a.requests; b0 += 32) total += b0 + lane < a.requests ? tiles_of(a, b0 + lane) : 0;
+        // the line's length, and where this part begins on it; a lane keeps the
+        // tiles of its first requests, so that most calls read the lengths once
+        int total = 0, kept[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) kept[k] = 32 * k + lane < a.requests ? tiles_of(a, 32 * k + lane) : 0, total += kept[k];
+        for (int b0 = 128; b0 < a.requests; b0 += 32) total += b0 + lane < a.requests ? tiles_of(a, b0 + lane) : 0;
         total = (int)__reduce_add_sync(~0u, (unsigned)total);
         const int begin = begin_of(total, parts_of(a, total), part);
         int seen = 0;
-        for (int b0 = 0; b0 < a.requests; b0 += 32) {
-            const int n = b0 + lane < a.requests ? tiles_of(a, b0 + lane) : 0;
+        auto place = [&](int b0, int n) {
             int incl = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -140,16 +144,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
             if (n && begin >= at && begin < at + n) bars->first_request = b0 + lane, bars->first_tile = begin - at;
             if (blockIdx.x == 0 && b0 + lane < a.requests) a.first[b0 + lane] = at;
             seen += __shfl_sync(~0u, incl, 31);
-        }
+        };
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (32 * k < a.requests) place(32 * k, kept[k]);
+        for (int b0 = 128; b0 < a.requests; b0 += 32) place(b0, b0 + lane < a.requests ? tiles_of(a, b0 + lane) : 0);
         if (lane == 0) {
             bars->total = total;
             if (blockIdx.x == 0) a.first[a.requests] = total;
             for (int s = 0; s < a.stages; ++s) {
                 bar_init(smem_addr(&bars->full[s]), 1);
-                bar_init(smem_addr(&bars->empty[s][0]), 1);
-                bar_init(smem_addr(&bars->empty[s][1]), 1);
+                bar_init(smem_addr(&bars->empty[s][0]), a.pair ? 2 : 1);
+                bar_init(smem_addr(&bars->empty[s][1]), a.pair ? 2 : 1);
             }
-            bar_init(smem_addr(&bars->q_full), 64);
+            bar_init(smem_addr(&bars->q_full), a.q_flat ? 1 : 64);
             bar_init(smem_addr(&bars->q_empty), 1);
             for (int s = 0; s < Z::scores; ++s) bar_init(smem_addr(&bars->s_ready[s]), 1);
             for (int s = 0; s < Z::weights; ++s) {
@@ -161,8 +169,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
         }
     }
     if (warp == kSoftWarps) tmem_alloc(smem_addr(&bars->tmem), kCols);
+    if (warp == kSoftWarps + 1 && lane == 0) fetch_map(&m_cache), fetch_map(&m_q);
+    __syncwarp();
     tmem_before_sync();
-    __syncthreads();
+    if (a.pair) cluster_sync();
+    else __syncthreads();
     tmem_after_sync();
     const uint32_t tmem = bars->tmem;
     const int parts = parts_of(a, bars->total);
@@ -194,7 +205,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
                 const uint32_t parity = (round & 1) ^ 1, full = smem_addr(&bars->full[s]);
                 const uint32_t dst = stage_at + s * stage_bytes + group * run * 128;
                 auto copy = [&](int c) {
-                    if (a.scattered) copy_rows_4(dst + c * Z::block_bytes, &m_cache, 64 * c, row[0], row[1], row[2], row[3], full);
+                    if (a.pair) {  // even column blocks by the first block of the pair, odd ones by the second
+                        if ((c & 1) == (int)(blockIdx.x & 1)) copy_box_2d_pair(dst + c * Z::block_bytes, &m_cache, 64 * c, row[0], full);
+                    } else if (a.scattered) copy_rows_4(dst + c * Z::block_bytes, &m_cache, 64 * c, row[0], row[1], row[2], row[3], full);
                     else copy_box_2d(dst + c * Z::block_bytes, &m_cache, 64 * c, row[0], full);
                 };
                 bar_wait(smem_addr(&bars->empty[s][0]), parity, dead);
@@ -207,8 +220,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
                 if (++s == a.stages) s = 0, ++round;
             }
         }
-    } else if (warp >= kSoftWarps + 2) {
+    } else if (warp >= kSoftWarps + 2 && a.q_flat) {
         // ----------------------------------------------------- query copies
+        for (int k = 0; more && warp == kSoftWarps + 2 && lane == 0; more = pc.next(a), ++k) {
+            const uint32_t full = smem_addr(&bars->q_full);
+            bar_wait(smem_addr(&bars->q_empty), (k & 1) ^ 1, dead);
+            bar_expect(full, blocks * q_block);
+            for (int c = 0; c < blocks; ++c) copy_box_3d(q_at + c * q_block, &m_q, 64 * c, rt * kRows, pc.b, full);
+        }
+    } else if (warp >= kSoftWarps + 2) {
+        // the same for queries whose (token, head) rows are not evenly spaced:
         // eight lanes a row of 128 bytes; the two warps take every second group of four rows
         const int r0 = (warp - kSoftWarps - 2) * 4 + lane / 8, col = 8 * (lane % 8), n = a.q_pad / 8;
         int64_t from[8];
@@ -250,6 +271,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
                 for (int k = 0; k < 4; ++k) product_ss<kHigh, kHigh>(d, q_low + 2 * k, c_low + 2 * k, word_s, c + k > 0);
             product_commit(smem_addr(&bars->s_ready[i % Z::scores]));
         };
+        auto release = [&](uint32_t bar) {
+            if (a.pair) product_commit_pair(bar);
+            else product_commit(bar);
+        };
         auto weighted = [&](int i, int s, bool add) {
             const int w = i % Z::weights;
             const uint32_t w_low = operand_low(p_at + w * (TILE * 2), 16);
@@ -259,9 +284,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
 #pragma unroll
                 for (int e = 0; e < TILE / 16; ++e)
                     product_ss<kHigh, kHigh>(tmem + 64 * c, w_low + 2 * e, c_low + 128 * e, word, add || e > 0);
-                if (c == 0) product_commit(smem_addr(&bars->empty[s][0]));
+                if (c == 0) release(smem_addr(&bars->empty[s][0]));
             }
-            product_commit(smem_addr(&bars->empty[s][1]));
+            release(smem_addr(&bars->empty[s][1]));
             product_commit(smem_addr(&bars->pv_done[w]));
         };
         // Scores run ahead of the weighted sums by as many tiles as there are
@@ -312,11 +337,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
         const int r0 = warp * 16 + lane / 4;  // this thread's rows: r0 and r0 + 8
         int see0 = 0, see1 = 0;
         const int f0 = rt * kRows + r0, f1 = f0 + 8;
-        const int tok0 = f0 / a.heads, tok1 = f1 / a.heads, h0 = f0 - tok0 * a.heads, h1 = f1 - tok1 * a.heads;
+        const int tok0 = f0 / a.heads, tok1 = f1 / a.heads;
         const bool real0 = tok0 < a.new_tokens, real1 = tok1 < a.new_tokens;
         // where P goes: row r, 16-byte chunk (k ^ r % 8), 4 bytes of it
         const uint32_t p0 = p_at + r0 * 128 + (lane % 4) * 4, p1 = p0 + 8 * 128;
         const int swz = r0 & 7;
+        // the rows this lane writes out at the end of a piece, 16 bytes of each
+        int64_t to[4];
+        uint32_t leaves = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int flat = rt * kRows + warp * 16 + 4 * k + lane / 8, tok = flat / a.heads;
+            if (tok < a.new_tokens) leaves |= 1u << k;
+            to[k] = tok * a.out_token + (flat - tok * a.heads) * a.out_head + 8 * (lane % 8);
+        }
         int i = 0, stage_of = 0;
         for (int k = 0; more; more = pc.next(a), ++k) {
             const int tokens = tokens_of(a, pc.b);
@@ -421,23 +455,51 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
             // an unfinished piece: the part's last if it begins the request, else its first
             const int64_t slot = (int64_t)blockIdx.x * 2 + (pc.t0 == 0);
             const float inv0 = sum0 > 0.f ? 1.f / sum0 : 0.f, inv1 = sum1 > 0.f ? 1.f / sum1 : 0.f;
-            T *out0 = (T *)a.out + (real0 ? pc.b * a.out_request + tok0 * a.out_token + h0 * a.out_head : 0);
-            T *out1 = (T *)a.out + (real1 ? pc.b * a.out_request + tok1 * a.out_token + h1 * a.out_head : 0);
-            float *sums = a.sums + (slot * kRows + r0) * a.rank;
+            float *sums = a.sums + (slot * kRows + warp * 16) * a.rank;
+            T *out = (T *)a.out + pc.b * a.out_request;
+            // Fragments hold 8 bytes of a row; through the (now idle) rows of P
+            // they leave as 128 bytes of a row.  A warp has 16 rows of its own there.
             for (int c = 0; c < value_blocks; ++c) {
                 uint32_t o[32];
                 float *v = (float *)o;
                 tmem_ld_rows<64>(o_at + 64 * c, o);
                 tmem_wait_ld();
-                const int col = 64 * c + 2 * (lane % 4);
+                if (whole) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (whole) {
-                        if (real0) *(uint32_t *)(out0 + col + 8 * e) = sum0 > 0.f ? pack2<T>(v[4 * e] * inv0, v[4 * e + 1] * inv0) : 0u;
-                        if (real1) *(uint32_t *)(out1 + col + 8 * e) = sum1 > 0.f ? pack2<T>(v[4 * e + 2] * inv1, v[4 * e + 3] * inv1) : 0u;
-                    } else {
-                        if (real0) *(float2 *)(sums + col + 8 * e) = make_float2(v[4 * e], v[4 * e + 1]);
-                        if (real1) *(float2 *)(sums + 8 * a.rank + col + 8 * e) = make_float2(v[4 * e + 2], v[4 * e + 3]);
+                    for (int e = 0; e < 8; ++e) {
+                        const uint32_t chunk = (uint32_t)((e ^ swz) << 4);
+                        const uint32_t w0 = sum0 > 0.f ? pack2<T>(v[4 * e] * inv0, v[4 * e + 1] * inv0) : 0u;
+                        const uint32_t w1 = sum1 > 0.f ? pack2<T>(v[4 * e + 2] * inv1, v[4 * e + 3] * inv1) : 0u;
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(p0 + chunk), "r"(w0) : "memory");
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(p1 + chunk), "r"(w1) : "memory");
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int r = 4 * k + lane / 8;
+                        const uint4 w = *(const uint4 *)(smem + p_offset + (warp * 16 + r) * 128 + (((lane % 8) ^ (r & 7)) << 4));
+                        if (leaves >> k & 1) *(uint4 *)(out + to[k] + 64 * c) = w;
+                    }
+                    __syncwarp();
+                } else {
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        const int turn = (r0 & 3) << 1 | (r0 >> 2 & 1);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t at = (uint32_t)(((2 * e + (lane % 4) / 2) ^ turn) << 4 | (lane & 1) << 3);
+                            const float *x = v + 16 * hf + 4 * e;
+                            asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(p_at + r0 * 128 + at), "f"(x[0]), "f"(x[1]) : "memory");
+                            asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(p_at + (r0 + 8) * 128 + at), "f"(x[2]), "f"(x[3]) : "memory");
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int r = 4 * k + lane / 8, tr = (r & 3) << 1 | (r >> 2 & 1);
+                            const uint4 w = *(const uint4 *)(smem + p_offset + (warp * 16 + r) * 128 + (((lane % 8) ^ tr) << 4));
+                            if (leaves >> k & 1) *(uint4 *)(sums + r * a.rank + 64 * c + 32 * hf + 4 * (lane % 8)) = w;
+                        }
+                        __syncwarp();
                     }
                 }
             }
@@ -455,83 +517,87 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
             }
         }
     }
+    __syncwarp();
     tmem_before_sync();
-    __syncthreads();
+    if (a.pair) cluster_sync();  // the other block's copies and arrivals have come
+    else __syncthreads();
     if (warp == kSoftWarps) tmem_free(tmem, kCols);
 }
 
-// Joins the pieces of the requests that were cut: one block a row, in the
-// order of the parts, so that the result does not depend on timing.  Requests
-// without a cached token get their zeros here.
-constexpr int kJoinThreads = 256;
+// Joins the pieces of the requests that were cut, in the order of the parts,
+// so that the result does not depend on timing.  Requests without a cached token
+// get their zeros here.  WARPS warps share a row, each taking every WARPS-th piece.
+constexpr int kJoinWarps = 8;
 
-template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) k_join(const __grid_constant__ Args a) {
-    __shared__ float weight[kJoinThreads], share[kJoinThreads];
-    __shared__ float4 part[kJoinThreads];
+template <typename T, int WARPS> __global__ void __launch_bounds__(kJoinWarps * 32) k_join(const __grid_constant__ Args a) {
+    __shared__ float4 sum_of[WARPS > 1 ? kJoinWarps : 1][SIM_OP_MAX_RANK / 4];
     asm volatile("griddepcontrol.wait;" ::: "memory");  // the parts are written
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, mine = warp % WARPS;
     const int rows = a.new_tokens * a.heads;
-    const int b = blockIdx.x / rows, f = blockIdx.x - b * rows;
+    const int64_t row = (int64_t)blockIdx.x * (kJoinWarps / WARPS) + warp / WARPS;
+    if (row >= (int64_t)a.requests * rows) return;
+    const int b = (int)(row / rows), f = (int)(row - (int64_t)b * rows);
     const int tok = f / a.heads, h = f - tok * a.heads, rt = f / kRows, r = f % kRows;
     const int first = a.first[b], past = a.first[b + 1], total = a.first[a.requests];
     T *out = (T *)a.out + b * a.out_request + tok * a.out_token + h * a.out_head;
     if (first == past) {
-        for (int i = threadIdx.x * 8; i < a.rank; i += kJoinThreads * 8) *(uint4 *)(out + i) = make_uint4(0, 0, 0, 0);
-        if (a.lse && threadIdx.x == 0) a.lse[blockIdx.x] = -INFINITY;
+        if (mine == 0) {
+            for (int i = lane * 8; i < a.rank; i += 256) *(uint4 *)(out + i) = make_uint4(0, 0, 0, 0);
+            if (a.lse && lane == 0) a.lse[row] = -INFINITY;
+        }
         return;
     }
     // the parts that hold tiles [first, past)
     const int parts = parts_of(a, total);
     auto part_of = [&](int tile) { return (int)((((int64_t)tile + 1) * parts - 1) / total); };
-    const int l0 = part_of(first), l1 = part_of(past - 1);
-    if (l0 == l1) return;
-    const int n = l1 - l0 + 1;
-    auto stat = [&](int l) { return a.stats[(((int64_t)(l * a.row_tiles + rt)) * 2 + (l == l0)) * kRows + r]; };
+    const int l0 = part_of(first), n = part_of(past - 1) - l0 + 1;
+    if (n == 1) return;
+    // piece l of the request: the last of its part where the request begins there, else the first
+    auto slot = [&](int l) { return (((int64_t)(l0 + l) * a.row_tiles + rt) * 2 + (l == 0)) * kRows + r; };
     float m = -INFINITY;
-    for (int l = threadIdx.x; l < n; l += kJoinThreads) m = fmaxf(m, stat(l0 + l).x);
-    weight[threadIdx.x] = m;
-    __syncthreads();
-    for (int o = kJoinThreads / 2; o; o >>= 1) {
-        if (threadIdx.x < o) weight[threadIdx.x] = fmaxf(weight[threadIdx.x], weight[threadIdx.x + o]);
-        __syncthreads();
-    }
-    m = weight[0];
-    // `groups` threads share four columns, each taking every groups-th piece
-    const int quads = a.rank / 4, groups = kJoinThreads / quads, g = threadIdx.x / quads, c = threadIdx.x % quads;
-    float total_w = 0.f;
-    float4 v = make_float4(0, 0, 0, 0);
-    for (int base = 0; base < n; base += kJoinThreads) {
-        __syncthreads();
-        if (base + (int)threadIdx.x < n) {
-            const float2 st = stat(l0 + base + threadIdx.x);
-            const float w = st.x == -INFINITY ? 0.f : exp2_fast(st.x - m);
-            weight[threadIdx.x] = w, share[threadIdx.x] = w * st.y;
+    for (int l = lane; l < n; l += 32) m = fmaxf(m, a.stats[slot(l)].x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    float all = 0.f;
+    float4 v[4] = {};
+    for (int l1 = 0; l1 < n; l1 += 32) {
+        const float2 st = l1 + lane < n ? a.stats[slot(l1 + lane)] : make_float2(-INFINITY, 0.f);
+        const float w = st.x == -INFINITY ? 0.f : exp2_fast(st.x - m);
+        all += warp_sum(w * st.y);
+        const int k = min(32, n - l1);
+#pragma unroll 4
+        for (int l = mine; l < k; l += WARPS) {
+            const float wl = __shfl_sync(~0u, w, l);
+            const float *x = a.sums + slot(l1 + l) * a.rank + 4 * lane;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (128 * j + 4 * lane < a.rank) {
+                    const float4 u = *(const float4 *)(x + 128 * j);
+                    v[j].x += wl * u.x, v[j].y += wl * u.y, v[j].z += wl * u.z, v[j].w += wl * u.w;
+                }
         }
-        __syncthreads();
-        const int k = min(kJoinThreads, n - base);
-        for (int l = 0; l < k; ++l) total_w += share[l];
-        if (g < groups)
-            for (int l = g; l < k; l += groups) {
-                const int p = l0 + base + l;
-                const float w = weight[l];
-                const float4 x =
-                    *(const float4 *)(a.sums + ((((int64_t)(p * a.row_tiles + rt)) * 2 + (p == l0)) * kRows + r) * a.rank + 4 * c);
-                v.x += w * x.x, v.y += w * x.y, v.z += w * x.z, v.w += w * x.w;
+    }
+    if (WARPS > 1) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum_of[warp][lane + 32 * j] = v[j];
+        __syncthreads();  // WARPS is the whole block: no warp of it has left
+        if (mine) return;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            for (int k = 1; k < WARPS; ++k) {
+                const float4 u = sum_of[k][lane + 32 * j];
+                v[j].x += u.x, v[j].y += u.y, v[j].z += u.z, v[j].w += u.w;
             }
     }
-    part[threadIdx.x] = v;
-    __syncthreads();
-    if (g == 0) {
-        for (int k = 1; k < groups; ++k) {
-            const float4 x = part[k * quads + c];
-            v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+    const float inv = all > 0.f ? 1.f / all : 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (128 * j + 4 * lane < a.rank) {
+            uint2 w = make_uint2(0, 0);
+            if (all > 0.f) w = make_uint2(pack2<T>(v[j].x * inv, v[j].y * inv), pack2<T>(v[j].z * inv, v[j].w * inv));
+            *(uint2 *)(out + 128 * j + 4 * lane) = w;
         }
-        const float inv = total_w > 0.f ? 1.f / total_w : 0.f;
-        uint2 w = make_uint2(0, 0);
-        if (total_w > 0.f) w = make_uint2(pack2<T>(v.x * inv, v.y * inv), pack2<T>(v.z * inv, v.w * inv));
-        *(uint2 *)(out + 4 * c) = w;
-    }
-    if (a.lse && threadIdx.x == 0) a.lse[blockIdx.x] = total_w > 0.f ? (m + log2f(total_w)) * 0.6931471805599453f : -INFINITY;
+    if (a.lse && lane == 0) a.lse[row] = all > 0.f ? (m + log2f(all)) * 0.6931471805599453f : -INFINITY;
 }
 
 // How the work is cut: row tiles side by side, and parts of the line of tiles.
@@ -553,22 +619,32 @@ Cut cut_for(int sms, int64_t requests, int64_t new_tokens, int64_t heads, int64_
     return c;
 }
 
-template <typename T> int run(const Args &k, const CUtensorMap &m, const Cut &c, cudaStream_t st) {
+template <typename T> int run(const Args &k, const CUtensorMap &m_cache, const CUtensorMap &m_q, const Cut &c, cudaStream_t st) {
     auto kernel = k.tile == 32 ? k_decode<T, 32> : k_decode<T, 64>;
     if (!allow_shared(kernel, kShared)) return SIM_ERR_CUDA;
-    kernel<<<c.row_tiles * c.lanes, kThreads, kShared, st>>>(k, m);
-    const int rc = launched("sim_op_latent_decode");
-    if (rc) return rc;
-    // the join's blocks start while the last parts run, and wait for them
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(k.requests * k.new_tokens * k.heads);
-    cfg.blockDim = dim3(kJoinThreads);
-    cfg.stream = st;
     cudaLaunchAttribute at[1];
+    cfg.gridDim = dim3(c.row_tiles * c.lanes);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kShared;
+    cfg.stream = st;
+    cfg.attrs = at, cfg.numAttrs = k.pair ? 1 : 0;
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, k, m_cache, m_q);
+    if (e != cudaSuccess) return fail(SIM_ERR_CUDA, "sim_op_latent_decode: %s", cudaGetErrorString(e));
+    // A row has about lanes / requests pieces: many are shared by a block's
+    // warps, few are one warp's.  The join's blocks start while the last parts run,
+    // and wait for them.
+    const bool many = c.lanes > 8 * (int64_t)k.requests;
+    const int64_t rows = (int64_t)k.requests * k.new_tokens * k.heads, per = many ? 1 : kJoinWarps;
+    cfg.gridDim = dim3((unsigned)((rows + per - 1) / per));
+    cfg.blockDim = dim3(kJoinWarps * 32);
+    cfg.dynamicSmemBytes = 0;
+    cfg.numAttrs = 1;
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at, cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_join<T>, k);
+    e = cudaLaunchKernelEx(&cfg, many ? k_join<T, kJoinWarps> : k_join<T, 1>, k);
     return e == cudaSuccess ? SIM_OK : fail(SIM_ERR_CUDA, "sim_op_latent_decode (join): %s", cudaGetErrorString(e));
 }
 
@@ -637,7 +713,7 @@ extern "C" int sim_op_latent_decode(const sim_op_latent_decode_t *a, void *strea
     k.scale_log2 = std::fmax(std::fabs(a->scale) * 1.4426950408889634f, 1e-30f);  // not 0: a masked score is -infinity times it
     k.negative = a->scale < 0;
     const bool bf = a->type == SIM_OP_BF16;
-    CUtensorMap m;
+    CUtensorMap m, mq;
     const uint64_t size[2] = {(uint64_t)k.width, (uint64_t)k.none};
     const int64_t stride[1] = {a->blocks ? a->cache_row : k.width};
     // One row tile: bound by memory, and 5 stages of 32 tokens keep more in
@@ -654,6 +730,16 @@ extern "C" int sim_op_latent_decode(const sim_op_latent_decode_t *a, void *strea
     k.scattered = a->block_tokens % 4 != 0;
     const uint32_t box[2] = {64, k.scattered ? 1u : (uint32_t)k.run};
     if (!box_map(&m, a->blocks ? a->cache : a->q, bf, 2, size, stride, box)) return SIM_ERR_CUDA;
+    // Q's (token, head) rows as one line
+    const int64_t q_row = a->heads > 1 ? a->q_head : a->q_token;
+    k.q_flat = a->new_tokens == 1 || a->heads == 1 || a->q_token == a->heads * a->q_head;
+    {
+        const uint64_t size[3] = {(uint64_t)k.width, (uint64_t)most_rows, (uint64_t)a->requests};
+        const int64_t stride[2] = {most_rows > 1 && k.q_flat ? q_row : 8, a->requests > 1 ? a->q_request : 8};
+        const uint32_t box[3] = {64, (uint32_t)k.q_pad, 1};
+        if (!box_map(&mq, a->q, bf, 3, size, stride, box)) return SIM_ERR_CUDA;
+    }
+    k.pair = c.row_tiles % 2 == 0 && !k.scattered;
     const cudaStream_t st = (cudaStream_t)stream;
-    return bf ? run<__nv_bfloat16>(k, m, c, st) : run<__half>(k, m, c, st);
+    return bf ? run<__nv_bfloat16>(k, m, mq, c, st) : run<__half>(k, m, mq, c, st);
 }

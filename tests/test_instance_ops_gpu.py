@@ -231,7 +231,8 @@ def check_decode(q, cache, table, lengths, rank, scale, out, lse):
     ([1], 1, 1, 512, 64, 16), ([0], 1, 16, 512, 64, 16), ([0, 5, 0, 1], 1, 16, 512, 64, 16), ([63, 64, 65, 127, 128, 129], 1, 16, 512, 64, 16),
     ([777], 1, 16, 512, 64, 16), ([300, 2, 1000], 1, 128, 512, 64, 16), ([200, 31], 1, 65, 512, 64, 12), ([500], 1, 64, 256, 32, 7),
     ([90, 400], 3, 16, 512, 64, 64), ([2, 5, 1], 5, 3, 512, 64, 16), ([64, 65, 66], 4, 17, 128, 64, 1), ([333], 1, 130, 512, 0, 16),
-    ([1025, 17], 2, 40, 64, 8, 48), ([3000], 1, 20, 512, 64, 16), ([40] * 70, 1, 5, 192, 40, 16), ([4100, 1, 0, 2500, 64], 7, 10, 512, 64, 33)])
+    ([1025, 17], 2, 40, 64, 8, 48), ([3000], 1, 20, 512, 64, 16), ([40] * 70, 1, 5, 192, 40, 16), ([4100, 1, 0, 2500, 64], 7, 10, 512, 64, 33),
+    ([k * 7 % 90 for k in range(300)], 1, 4, 128, 64, 16), ([700, 130], 2, 96, 512, 64, 32), ([500, 0, 77], 4, 64, 256, 64, 24)])
 def test_decode(lengths, new, heads, rank, key_dim, block, dtype):
     q, cache, table, n = decode_case(lengths, new, heads, rank, key_dim, block, dtype, seed=len(lengths) + heads)
     scale = 1.7 / math.sqrt(rank + key_dim)
