@@ -621,7 +621,8 @@ Cut cut_for(int sms, int64_t requests, int64_t new_tokens, int64_t heads, int64_
 
 template <typename T> int run(const Args &k, const CUtensorMap &m_cache, const CUtensorMap &m_q, const Cut &c, cudaStream_t st) {
     auto kernel = k.tile == 32 ? k_decode<T, 32> : k_decode<T, 64>;
-    if (!allow_shared(kernel, kShared)) return SIM_ERR_CUDA;
+    static std::atomic<uint64_t> told[2];
+    if (!allow_shared((const void *)kernel, kShared, told[k.tile == 32])) return SIM_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
     cfg.gridDim = dim3(c.row_tiles * c.lanes);

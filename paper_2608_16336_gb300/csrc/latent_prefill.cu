@@ -322,7 +322,8 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
 
 template <typename T>
 int run(const sim_op_latent_prefill_t *a, const Args &k, const CUtensorMap *m, unsigned grid, cudaStream_t st) {
-    if (!allow_shared(k_prefill<T>, kShared)) return SIM_ERR_CUDA;
+    static std::atomic<uint64_t> told;
+    if (!allow_shared((const void *)k_prefill<T>, kShared, told)) return SIM_ERR_CUDA;
     k_prefill<T><<<grid, kThreads, kShared, st>>>(k, m[0], m[1], m[2], m[3], m[4]);
     return launched("sim_op_latent_prefill");
 }

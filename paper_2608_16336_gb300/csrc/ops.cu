@@ -36,6 +36,20 @@ int sm_count() {
     return n;
 }
 
+bool allow_shared(const void *kernel, int bytes, std::atomic<uint64_t> &done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (e == cudaSuccess && (done.load(std::memory_order_relaxed) & bit)) return true;
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) {
+        fail(SIM_ERR_CUDA, "shared memory: %s", cudaGetErrorString(e));
+        return false;
+    }
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+
 bool box_map(CUtensorMap *map, const void *base, bool bf16, int dims, const uint64_t *size, const int64_t *stride, const uint32_t *box) {
     static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> encode{nullptr};
     PFN_cuTensorMapEncodeTiled_v12000 f = encode.load(std::memory_order_acquire);

@@ -5,6 +5,8 @@
 
 #include "mtsim_ops.h"
 
+#include <atomic>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -19,6 +21,9 @@ inline int launched(const char *what) {
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? SIM_OK : fail(SIM_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
+
+// Lets a kernel use that much shared memory; `done` (one a kernel) keeps which devices have been told.
+bool allow_shared(const void *kernel, int bytes, std::atomic<uint64_t> &done);
 
 // SMs of the current device (152 on a whole GB300), or 0 with an error set.
 int sm_count();
@@ -39,19 +44,56 @@ template <> struct elem<__half> {
     static __device__ __half from(float v) { return __float2half(v); }
 };
 
+// 16 bytes of a row, and their elements in 32 bits.
+template <typename T> struct alignas(16) Vec {
+    static constexpr int N = 16 / sizeof(T);
+    T v[N];
+    __device__ __forceinline__ void to(float *f) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = elem<T>::to(v[i]);
+    }
+    __device__ __forceinline__ void from(const float *f);
+};
+template <> __device__ __forceinline__ void Vec<float>::from(const float *f) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = f[i];
+}
+template <> __device__ __forceinline__ void Vec<__nv_bfloat16>::from(const float *f) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) *(__nv_bfloat162 *)(v + i) = __floats2bfloat162_rn(f[i], f[i + 1]);
+}
+template <> __device__ __forceinline__ void Vec<__half>::from(const float *f) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) *(__half2 *)(v + i) = __floats2half2_rn(f[i], f[i + 1]);
+}
+
 // Cosine and sine of position * frequency.  The angle in turns, modulo one,
 // is position * (frequency / 2 pi * 2^64) in 64-bit wrapping integers: exact
 // reduction at any position, one 64-bit multiplication an angle, and what is left is
-// rounded once to 32 bits in [-1/2, 1/2) turns.
+// rounded once to 32 bits in [-1/2, 1/2) turns.  The factor is the frequency's
+// 53-bit whole number times 2^66 / 2 pi, shifted by its exponent (64-bit
+// floating point runs at a sixty-fourth of the rate here).
 __device__ __forceinline__ unsigned long long turns_per_position(double frequency) {
-    const double t = frequency * 0.15915494309189533577;  // 1 / (2 pi)
-    return __double2ull_rn((t - floor(t)) * 18446744073709551616.0);
+    const unsigned long long b = (unsigned long long)__double_as_longlong(frequency);
+    const int e = (int)(b >> 52) & 0x7FF;
+    const unsigned long long m = (b & 0xFFFFFFFFFFFFFull) | (e ? 1ull << 52 : 0);
+    const unsigned long long c = 0xA2F9836E4E44152Aull;  // round(2^66 / 2 pi)
+    const unsigned long long lo = m * c, hi = __umul64hi(m, c);
+    const int right = 1077 - (e ? e : 1);  // (hi, lo) = turns * 2^64 * 2^right
+    unsigned long long t;
+    if (right <= 0) t = right > -64 ? lo << -right : 0;
+    else if (right < 64) t = hi << (64 - right) | lo >> right;
+    else t = right < 128 ? hi >> (right - 64) : 0;
+    return b >> 63 ? 0 - t : t;
 }
 
 __device__ __forceinline__ void angle_cos_sin(unsigned long long turns, long long position, float &c, float &s) {
     const long long at = (long long)(turns * (unsigned long long)position);
     sincospif((float)(int)(at >> 32) * 4.656612873077393e-10f /* 2^-31: half turns */, &s, &c);
 }
+
+// Barrier `id` of the block's first (or other) `threads` threads.
+__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll

@@ -750,8 +750,8 @@ template <typename T> int run(const sim_op_sample_t *a, cudaStream_t st) {
     const int warp_len = stretch(blocks);
     const int64_t bytes = (int64_t)warp_len * kWarps * sizeof(T);
     const bool staged = bytes <= kMostStaged;
-    const cudaError_t s = cudaFuncSetAttribute(k_sample<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostStaged);
-    if (s != cudaSuccess) return fail(SIM_ERR_CUDA, "sim_op_sample: %s", cudaGetErrorString(s));
+    static std::atomic<uint64_t> told;
+    if (!allow_shared((const void *)k_sample<T>, kMostStaged, told)) return SIM_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
     cfg.gridDim = dim3((unsigned)a->rows * blocks);

@@ -246,13 +246,6 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
 // driver refuses it.  strides: elements, of dimensions 1 and up.
 bool box_map(CUtensorMap *map, const void *base, bool bf16, int dims, const uint64_t *size, const int64_t *stride, const uint32_t *box);
 
-// Lets a kernel use that much shared memory, once per device.
-template <typename K> bool allow_shared(K kernel, int bytes) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != cudaSuccess) fail(SIM_ERR_CUDA, "shared memory: %s", cudaGetErrorString(e));
-    return e == cudaSuccess;
-}
-
 }  // namespace mtop
 
 #endif

@@ -43,6 +43,7 @@ EXPORTS = ["sim_op_rotary", "sim_op_latent_append", "sim_op_latent_decode", "sim
            "sim_op_latent_prefill", "sim_op_sample", "sim_op_faults", "sim_op_last_error"]
 
 _LIB = None
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
 
@@ -80,11 +81,13 @@ def _place(*tensors) -> int:
     """The one CUDA device, the current one, that every tensor is on."""
     device = tensors[0].get_device()
     for t in tensors:
-        if t.get_device() != device or device < 0:
+        if t.get_device() != device:
             raise ValueError("every tensor must be on the same CUDA device")
         if t.requires_grad and torch.is_grad_enabled():
             raise ValueError("forward only: call under torch.no_grad() or detach the tensors")
-    if device != torch.cuda.current_device():
+    if device < 0:
+        raise ValueError("the tensors must be on a CUDA device")
+    if device != _current_device():
         raise ValueError("the tensors are on cuda:%d, which is not the current device" % device)
     return device
 
@@ -325,20 +328,25 @@ def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=N
         out = torch.empty(rows, dtype=torch.int64, device=logits.device)
     if logprob is None:
         logprob = torch.empty(rows, dtype=torch.float32, device=logits.device)
-    given = [logits, out]
-    pointers = []
-    for name, t, dtype in (("uniform", uniform, torch.float32), ("temperature", temperature, torch.float32),
-                           ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32),
-                           ("out", out, torch.int64), ("logprob", logprob, torch.float32)):
+    code = _type("logits", logits)
+    device = logits.get_device()
+
+    def vector(name, t, dtype):
+        """The address of a vector of one value a row (0: none)."""
         if t is None:
-            pointers.append(0)
-            continue
+            return 0
         if t.dtype is not dtype:
             raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
-        _packed(name, t, (rows,))
-        given.append(t)
-        pointers.append(t.data_ptr())
-    code = _type("logits", logits)
-    device = _place(*given)
-    _check(lib().sim_op_sample(SAMPLE.pack(logits.data_ptr(), *pointers, stride, rows, vocab, code), _stream_of(device)))
+        if t.dim() != 1 or t.shape[0] != rows or not t.is_contiguous():
+            raise ValueError("%s must be a contiguous vector of %d values" % (name, rows))
+        if t.get_device() != device:
+            raise ValueError("every tensor must be on the same CUDA device")
+        return t.data_ptr()
+
+    real = torch.float32
+    args = SAMPLE.pack(logits.data_ptr(), vector("uniform", uniform, real), vector("temperature", temperature, real),
+                       vector("top_k", top_k, torch.int32), vector("top_p", top_p, real), vector("min_p", min_p, real),
+                       vector("out", out, torch.int64), vector("logprob", logprob, real), stride, rows, vocab, code)
+    _place(logits)
+    _check(lib().sim_op_sample(args, _stream_of(device)))
     return out, logprob
