@@ -19,7 +19,7 @@ constexpr int kTile = 128;
 constexpr int kSlotBytes = kTile * 128;
 constexpr int kSlots = 8;
 constexpr int kSoftWarps = 8;
-constexpr int kThreads = (kSoftWarps + 4) * 32;  // + products, copies, and two that only make up the warpgroup
+constexpr int kThreads = (kSoftWarps + 4) * 32;  // + products, copies, zeros, one idle
 // Registers a thread: 3 warpgroups launch with 168 (504 in all); the two of
 // weights take 224, which holds a row's 128 scores without spilling.
 constexpr int kSoftRegs = 224, kOtherRegs = 56;
@@ -44,8 +44,10 @@ struct Args {
     bool negative;
 };
 
+constexpr int kInFlight = 4;  // tiles of K (and of V) in the ring: a tile of each takes 2 slots or more
 struct Barriers {
-    uint64_t q_full, full[kSlots], empty[kSlots], s_ready[2], p_ready[2], o_ready[2];
+    uint64_t q_full, k_full[kInFlight], k_empty[kInFlight], v_full[kInFlight], v_empty[kInFlight];
+    uint64_t s_ready[2], p_ready[2], o_ready[2], v_cut, v_clean;  // v_cut: the last tile of V, if it has foreign rows
     uint32_t tmem;
 };
 
@@ -75,13 +77,18 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     const int sees0 = a.causal ? min(nk, last0 + nk - nq + 1) : nk, sees1 = a.causal ? min(nk, last1 + nk - nq + 1) : nk;
     const int n0 = sees0 > 0 ? (sees0 + kTile - 1) / kTile : 0, n1 = two && sees1 > 0 ? (sees1 + kTile - 1) / kTile : 0;
     const int n = max(n0, n1);
-    const int qk_blocks = a.head_blocks + a.key_blocks;
+    const int qk_blocks = a.head_blocks + a.key_blocks, per_tile = qk_blocks + a.value_blocks;
+    const bool cut = n * kTile > nk;  // the last tile has rows that are not the request's
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     bool dead = false;
     if (threadIdx.x == 0) {
         bar_init(smem_addr(&bars->q_full), 1);
-        for (int s = 0; s < kSlots; ++s) bar_init(smem_addr(&bars->full[s]), 1), bar_init(smem_addr(&bars->empty[s]), 1);
+        for (int s = 0; s < kInFlight; ++s) {
+            bar_init(smem_addr(&bars->k_full[s]), 1), bar_init(smem_addr(&bars->k_empty[s]), 1);
+            bar_init(smem_addr(&bars->v_full[s]), 1), bar_init(smem_addr(&bars->v_empty[s]), 1);
+        }
+        bar_init(smem_addr(&bars->v_cut), 1), bar_init(smem_addr(&bars->v_clean), 32);
         for (int t = 0; t < 2; ++t) {
             bar_init(smem_addr(&bars->s_ready[t]), 1);
             bar_init(smem_addr(&bars->p_ready[t]), kTile);
@@ -90,6 +97,8 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
         bar_init_done();
     }
     if (warp == kSoftWarps) tmem_alloc(smem_addr(&bars->tmem), kCols);
+    if (threadIdx.x == (kSoftWarps + 1) * 32) fetch_map(&m_q), fetch_map(&m_qr), fetch_map(&m_k), fetch_map(&m_kr), fetch_map(&m_v);
+    __syncwarp();
     tmem_before_sync();
     __syncthreads();
     tmem_after_sync();
@@ -108,107 +117,103 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
                     if (c < a.head_blocks) copy_box_3d(dst, &m_q, 64 * c, h, r, qf);
                     else copy_box_3d(dst, &m_qr, 64 * (c - a.head_blocks), h, r, qf);
                 }
-            int slot = 0;
-            uint32_t round = 0;
-            auto next = [&]() -> uint32_t {
-                bar_wait(smem_addr(&bars->empty[slot]), (round & 1) ^ 1, dead);
-                bar_expect(smem_addr(&bars->full[slot]), kSlotBytes);
-                return ring + slot * kSlotBytes;
+            // a slot is free when the tile it held eight slots ago has been used
+            auto slot_for = [&](int stream) -> uint32_t {
+                const int old = stream - kSlots;
+                if (old >= 0) {
+                    const int i = old / per_tile;
+                    uint64_t *empty = old - i * per_tile < qk_blocks ? bars->k_empty : bars->v_empty;
+                    bar_wait(smem_addr(&empty[i % kInFlight]), (i / kInFlight) & 1, dead);
+                }
+                return ring + stream % kSlots * kSlotBytes;
             };
-            auto took = [&]() {
-                if (++slot == kSlots) slot = 0, ++round;
-            };
+            int stream = 0;
             for (int i = 0; i < n; ++i) {
                 const int r = k0 + i * kTile;
-                for (int c = 0; c < qk_blocks; ++c, took()) {
-                    const uint32_t dst = next();
-                    if (c < a.head_blocks) copy_box_3d(dst, &m_k, 64 * c, h, r, smem_addr(&bars->full[slot]));
-                    else copy_box_2d(dst, &m_kr, 64 * (c - a.head_blocks), r, smem_addr(&bars->full[slot]));
+                const uint32_t kf = smem_addr(&bars->k_full[i % kInFlight]), vf = smem_addr(cut && i == n - 1 ? &bars->v_cut : &bars->v_full[i % kInFlight]);
+                for (int c = 0; c < qk_blocks; ++c, ++stream) {
+                    const uint32_t dst = slot_for(stream);
+                    if (c == 0) bar_expect(kf, qk_blocks * kSlotBytes);
+                    if (c < a.head_blocks) copy_box_3d(dst, &m_k, 64 * c, h, r, kf);
+                    else copy_box_2d(dst, &m_kr, 64 * (c - a.head_blocks), r, kf);
                 }
-                for (int c = 0; c < a.value_blocks; ++c, took()) {
-                    const uint32_t dst = next();
-                    copy_box_3d(dst, &m_v, 64 * c, h, r, smem_addr(&bars->full[slot]));
+                for (int c = 0; c < a.value_blocks; ++c, ++stream) {
+                    const uint32_t dst = slot_for(stream);
+                    if (c == 0) bar_expect(vf, a.value_blocks * kSlotBytes);
+                    copy_box_3d(dst, &m_v, 64 * c, h, r, vf);
                 }
             }
         }
+        if (warp == kSoftWarps + 2 && cut) {
+            // rows of the last tile past the request's keys hold another's values: zeros, so that 0 * NaN cannot appear
+            const int i = n - 1;
+            bar_wait(smem_addr(&bars->v_cut), 0, dead);
+            for (int c = 0; c < a.value_blocks; ++c) {
+                uint4 *rows_at = (uint4 *)(smem + (6 + (i * per_tile + qk_blocks + c) % kSlots) * kSlotBytes + (nk - i * kTile) * 128);
+                for (int e = lane; e < ((i + 1) * kTile - nk) * 8; e += 32) rows_at[e] = make_uint4(0, 0, 0, 0);
+            }
+            fence_async();
+            bar_arrive(smem_addr(&bars->v_clean));
+        }
         // -------------------------------------------------------- products
-        if (warp == kSoftWarps && n > 0) {
-            const bool bf = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value;
+        // One thread, and as few instructions as can be: what it executes
+        // between two products is time in which the tensor core runs dry.
+        if (warp == kSoftWarps && n > 0 && elect_one()) {
+            const bool bf = std::is_same<T, __nv_bfloat16>::value;
             const uint32_t word_s = product_word(kTile, kTile, bf, false, a.negative);
-            const uint32_t word_o = product_word(kTile, 64 * a.value_blocks, bf, true, false);
-            const int per_tile = qk_blocks + a.value_blocks;
-            auto slot_of = [&](int stream) { return stream % kSlots; };
-            auto wait_full = [&](int stream, int count) {
-                for (int c = 0; c < count; ++c)
-                    bar_wait(smem_addr(&bars->full[slot_of(stream + c)]), (uint32_t)((stream + c) / kSlots) & 1, dead);
-            };
-            auto release = [&](int stream, int count) {
-                for (int c = 0; c < count; ++c) product_commit(smem_addr(&bars->empty[slot_of(stream + c)]));
-            };
-            auto scores = [&](int t, int i) {  // S_t = Q_t K_i^T
-                const int stream = i * per_tile;
-                for (int c = 0; c < qk_blocks; ++c) {
-                    const uint32_t q_low = operand_low(q_at + (t * 3 + c) * kSlotBytes, 16),
-                                   k_low = operand_low(ring + slot_of(stream + c) * kSlotBytes, 16);
+            const uint32_t word_o = product_word(kTile, 64 * a.value_blocks, bf, true, false), word_h = product_word(kTile, 64, bf, true, false);
+            const uint32_t ring_k = operand_low(ring, 16), ring_v = operand_low(ring, kSlotBytes);
+            const uint32_t q_low[2] = {operand_low(q_at, 16), operand_low(q_at + 3 * kSlotBytes, 16)};
+            const uint32_t s_bar[2] = {smem_addr(&bars->s_ready[0]), smem_addr(&bars->s_ready[1])};
+            auto scores = [&](int t, int i, bool last) {  // S_t = Q_t K_i^T
+                int slot = i * per_tile;
+                uint32_t q = q_low[t];
+                for (int c = 0; c < qk_blocks; ++c, ++slot, q += kSlotBytes >> 4) {
+                    const uint32_t k = ring_k + (slot % kSlots) * (kSlotBytes >> 4);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        product_ss<kHigh, kHigh>(tmem + kColS + t * kTile, q_low + 2 * k, k_low + 2 * k, word_s, c + k > 0);
+                    for (int e = 0; e < 4; ++e)
+                        product_ss<kHigh, kHigh>(tmem + kColS + t * kTile, q + 2 * e, k + 2 * e, word_s, c + e > 0);
                 }
-                product_commit(smem_addr(&bars->s_ready[t]));
-                if (t == (i < n1 ? 1 : 0)) release(stream, qk_blocks);
+                product_commit(s_bar[t]);
+                if (last) product_commit(smem_addr(&bars->k_empty[i % kInFlight]));
             };
-            auto weighted = [&](int t, int i) {  // O_t += P_t V_i
-                const int stream = i * per_tile + qk_blocks;
-                if (a.value_blocks == 2 && slot_of(stream) == kSlots - 1) {
+            auto weighted = [&](int t, int i, bool last) {  // O_t += P_t V_i
+                const int slot = (i * per_tile + qk_blocks) % kSlots;
+                const uint32_t v = ring_v + slot * (kSlotBytes >> 4), o = tmem + kColO + t * kTile, p = tmem + kColS + t * kTile;
+                if (a.value_blocks == 2 && slot == kSlots - 1) {
                     // the two halves of V are not neighbours in the ring: one product each
-                    const uint32_t word_h = product_word(kTile, 64, bf, true, false);
-                    for (int c = 0; c < 2; ++c) {
-                        const uint32_t v_low = operand_low(ring + slot_of(stream + c) * kSlotBytes, kSlotBytes);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            product_ts<kHigh>(tmem + kColO + t * kTile + 64 * c, tmem + kColS + t * kTile + 8 * k, v_low + 128 * k, word_h,
-                                              i + k > 0);
-                    }
+                    for (int e = 0; e < 8; ++e) product_ts<kHigh>(o, p + 8 * e, v + 128 * e, word_h, i + e > 0);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) product_ts<kHigh>(o + 64, p + 8 * e, ring_v + 128 * e, word_h, i + e > 0);
                 } else {
-                    const uint32_t v_low = operand_low(ring + slot_of(stream) * kSlotBytes, kSlotBytes);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        product_ts<kHigh>(tmem + kColO + t * kTile, tmem + kColS + t * kTile + 8 * k, v_low + 128 * k, word_o, i + k > 0);
+                    for (int e = 0; e < 8; ++e) product_ts<kHigh>(o, p + 8 * e, v + 128 * e, word_o, i + e > 0);
                 }
-                if (t == (i < n1 ? 1 : 0)) release(stream, a.value_blocks);
-                if (i == (t ? n1 : n0) - 1) product_commit(smem_addr(&bars->o_ready[t]));
+                if (last) product_commit(smem_addr(&bars->v_empty[i % kInFlight]));
             };
             bar_wait(smem_addr(&bars->q_full), 0, dead);
-            wait_full(0, qk_blocks);
-            if (elect_one()) {
-                if (n0 > 0) scores(0, 0);
-                if (n1 > 0) scores(1, 0);
-            }
-            __syncwarp();
+            bar_wait(smem_addr(&bars->k_full[0]), 0, dead);
+            if (n0 > 0) scores(0, 0, n1 == 0);
+            if (n1 > 0) scores(1, 0, true);
             for (int i = 0; i < n; ++i) {
-                const int stream = i * per_tile + qk_blocks;
-                wait_full(stream, a.value_blocks);
-                if ((i + 1) * kTile > nk) {
-                    // rows past the request's keys hold another's values: zeros, so that 0 * NaN cannot appear
-                    for (int c = 0; c < a.value_blocks; ++c) {
-                        uint4 *rows_at = (uint4 *)(smem + (6 + slot_of(stream + c)) * kSlotBytes + (nk - i * kTile) * 128);
-                        for (int e = lane; e < ((i + 1) * kTile - nk) * 8; e += 32) rows_at[e] = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_async();
-                    __syncwarp();
-                }
-                for (int t = 0; t < 2; ++t) {
-                    const int nt = t ? n1 : n0;
-                    if (i >= nt) continue;
-                    bar_wait(smem_addr(&bars->p_ready[t]), (uint32_t)i & 1, dead);
+                if (cut && i == n - 1) bar_wait(smem_addr(&bars->v_clean), 0, dead);
+                else bar_wait(smem_addr(&bars->v_full[i % kInFlight]), (i / kInFlight) & 1, dead);
+                const bool more = i + 1 < n;
+                if (i < n0) {
+                    bar_wait(smem_addr(&bars->p_ready[0]), (uint32_t)i & 1, dead);
                     tmem_after_sync();
-                    if (elect_one()) weighted(t, i);
-                    __syncwarp();
-                    if (i + 1 < nt) {
-                        wait_full((i + 1) * per_tile, qk_blocks);
-                        if (elect_one()) scores(t, i + 1);
-                        __syncwarp();
-                    }
+                    weighted(0, i, i >= n1);
+                    if (i + 1 == n0) product_commit(smem_addr(&bars->o_ready[0]));
+                }
+                if (more) bar_wait(smem_addr(&bars->k_full[(i + 1) % kInFlight]), ((i + 1) / kInFlight) & 1, dead);
+                if (i + 1 < n0) scores(0, i + 1, i + 1 >= n1);
+                if (i < n1) {
+                    bar_wait(smem_addr(&bars->p_ready[1]), (uint32_t)i & 1, dead);
+                    tmem_after_sync();
+                    weighted(1, i, true);
+                    if (i + 1 == n1) product_commit(smem_addr(&bars->o_ready[1]));
+                    else scores(1, i + 1, true);
                 }
             }
         }
@@ -315,6 +320,7 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             }
         }
     }
+    __syncwarp();
     tmem_before_sync();
     __syncthreads();
     if (warp == kSoftWarps) tmem_free(tmem, kCols);
