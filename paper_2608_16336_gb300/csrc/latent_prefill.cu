@@ -3,6 +3,7 @@
 #include "tensor.cuh"
 
 #include <cmath>
+#include <cstddef>
 
 namespace mtop {
 namespace {
@@ -19,7 +20,7 @@ constexpr int kTile = 128;
 constexpr int kSlotBytes = kTile * 128;
 constexpr int kSlots = 8;
 constexpr int kSoftWarps = 8;
-constexpr int kThreads = (kSoftWarps + 4) * 32;  // + products, copies, zeros, one idle
+constexpr int kThreads = (kSoftWarps + 4) * 32;  // + products, copies of K, zeros, copies of V
 // Registers a thread: 3 warpgroups launch with 168 (504 in all); the two of
 // weights take 224, which holds a row's 128 scores without spilling.
 constexpr int kSoftRegs = 224, kOtherRegs = 56;
@@ -67,16 +68,18 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     item -= b * per_request;
     const int g0 = item / (a.row_blocks * a.group) * a.group, in_group = min(a.group, a.heads - g0);
     item -= g0 * a.row_blocks;
-    const int h = g0 + item % in_group, row0 = (a.row_blocks - 1 - item / in_group) * 2 * kTile;
+    const int h = g0 + item % in_group, base = (a.row_blocks - 1 - item / in_group) * 2 * kTile;
     const int q0 = min(max(a.q_offsets[b], 0), a.q_rows), q1 = min(a.q_offsets[b + 1], a.q_rows);
     const int k0 = min(max(a.k_offsets[b], 0), a.k_rows), k1 = min(a.k_offsets[b + 1], a.k_rows);
     const int nq = q1 - q0, nk = max(k1 - k0, 0), rows = min(nq, a.longest);
-    if (row0 >= rows) return;
-    const int last0 = min(row0 + kTile, rows) - 1, last1 = min(row0 + 2 * kTile, rows) - 1;
-    const bool two = row0 + kTile < rows;
-    const int sees0 = a.causal ? min(nk, last0 + nk - nq + 1) : nk, sees1 = a.causal ? min(nk, last1 + nk - nq + 1) : nk;
-    const int n0 = sees0 > 0 ? (sees0 + kTile - 1) / kTile : 0, n1 = two && sees1 > 0 ? (sees1 + kTile - 1) / kTile : 0;
-    const int n = max(n0, n1);
+    if (base >= rows) return;
+    const int start0 = base, start1 = base + kTile;
+    auto tiles_for = [&](int start) {  // of keys, for the rows from `start` on
+        if (start >= rows) return 0;
+        const int sees = a.causal ? min(nk, min(start + kTile, rows) + nk - nq) : nk;
+        return sees > 0 ? (sees + kTile - 1) / kTile : 0;
+    };
+    const int n0 = tiles_for(start0), n1 = tiles_for(start1), n = max(n0, n1);
     const int qk_blocks = a.head_blocks + a.key_blocks, per_tile = qk_blocks + a.value_blocks;
     const bool cut = n * kTile > nk;  // the last tile has rows that are not the request's
 
@@ -107,41 +110,38 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     if (warp >= kSoftWarps) {
         registers_down<kOtherRegs>();
         // ---------------------------------------------------------- copies
-        if (warp == kSoftWarps + 1 && lane == 0 && n > 0) {
+        // One warp for K (and Q), one for V, a lane a column block.  Eight slots
+        // earlier in the stream lies a block of a fixed kind, a fixed number of tiles
+        // back: when that has been used, the slot is free.
+        if (warp == kSoftWarps + 1 && lane < 6 && n > 0) {
             const uint32_t qf = smem_addr(&bars->q_full);
-            bar_expect(qf, (two ? 2 : 1) * qk_blocks * kSlotBytes);
-            for (int t = 0; t < (two ? 2 : 1); ++t)
-                for (int c = 0; c < qk_blocks; ++c) {
-                    const uint32_t dst = q_at + (t * 3 + c) * kSlotBytes;
-                    const int r = q0 + row0 + t * kTile;
-                    if (c < a.head_blocks) copy_box_3d(dst, &m_q, 64 * c, h, r, qf);
-                    else copy_box_3d(dst, &m_qr, 64 * (c - a.head_blocks), h, r, qf);
-                }
-            // a slot is free when the tile it held eight slots ago has been used
-            auto slot_for = [&](int stream) -> uint32_t {
-                const int old = stream - kSlots;
-                if (old >= 0) {
-                    const int i = old / per_tile;
-                    uint64_t *empty = old - i * per_tile < qk_blocks ? bars->k_empty : bars->v_empty;
-                    bar_wait(smem_addr(&empty[i % kInFlight]), (i / kInFlight) & 1, dead);
-                }
-                return ring + stream % kSlots * kSlotBytes;
-            };
-            int stream = 0;
-            for (int i = 0; i < n; ++i) {
-                const int r = k0 + i * kTile;
-                const uint32_t kf = smem_addr(&bars->k_full[i % kInFlight]), vf = smem_addr(cut && i == n - 1 ? &bars->v_cut : &bars->v_full[i % kInFlight]);
-                for (int c = 0; c < qk_blocks; ++c, ++stream) {
-                    const uint32_t dst = slot_for(stream);
-                    if (c == 0) bar_expect(kf, qk_blocks * kSlotBytes);
-                    if (c < a.head_blocks) copy_box_3d(dst, &m_k, 64 * c, h, r, kf);
-                    else copy_box_2d(dst, &m_kr, 64 * (c - a.head_blocks), r, kf);
-                }
-                for (int c = 0; c < a.value_blocks; ++c, ++stream) {
-                    const uint32_t dst = slot_for(stream);
-                    if (c == 0) bar_expect(vf, a.value_blocks * kSlotBytes);
-                    copy_box_3d(dst, &m_v, 64 * c, h, r, vf);
-                }
+            if (lane == 0) bar_expect(qf, ((n0 > 0) + (n1 > 0)) * qk_blocks * kSlotBytes);
+            const int t = lane / 3, c = lane % 3, r = q0 + (t ? start1 : start0);
+            const uint32_t dst = q_at + lane * kSlotBytes;
+            if (c < qk_blocks && (t ? n1 : n0) > 0) {
+                if (c < a.head_blocks) copy_box_3d(dst, &m_q, 64 * c, h, r, qf);
+                else copy_box_3d(dst, &m_qr, 64 * (c - a.head_blocks), h, r, qf);
+            }
+        }
+        if ((warp == kSoftWarps + 1 && lane < qk_blocks) || (warp == kSoftWarps + 3 && lane < a.value_blocks)) {
+            const bool of_v = warp == kSoftWarps + 3;
+            const int at = of_v ? qk_blocks + lane : lane;  // the block within a tile's blocks
+            const int back = (kSlots - at + per_tile - 1) / per_tile;  // the slot's last block: of tile i - back
+            const uint32_t empty = smem_addr(at - kSlots + back * per_tile < qk_blocks ? bars->k_empty : bars->v_empty);
+            const uint32_t full = smem_addr(of_v ? bars->v_full : bars->k_full);
+            const uint32_t bytes = (of_v ? a.value_blocks : qk_blocks) * kSlotBytes;
+            const bool of_shared_key = !of_v && lane >= a.head_blocks;
+            const CUtensorMap *map = of_v ? &m_v : of_shared_key ? &m_kr : &m_k;
+            const int x = 64 * (of_shared_key ? lane - a.head_blocks : lane);
+            int slot = at, r = k0;
+            for (int i = 0; i < n; ++i, r += kTile, slot = (slot + per_tile) % kSlots) {
+                const int old = i - back;
+                if (old >= 0) bar_wait(empty + old % kInFlight * 8, (old / kInFlight) & 1, dead);
+                const uint32_t bar = of_v && cut && i == n - 1 ? smem_addr(&bars->v_cut) : full + i % kInFlight * 8;
+                if (lane == 0) bar_expect(bar, bytes);
+                const uint32_t dst = ring + slot * kSlotBytes;
+                if (of_shared_key) copy_box_2d(dst, map, x, r, bar);
+                else copy_box_3d(dst, map, x, h, r, bar);
             }
         }
         if (warp == kSoftWarps + 2 && cut) {
@@ -156,71 +156,99 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             bar_arrive(smem_addr(&bars->v_clean));
         }
         // -------------------------------------------------------- products
-        // One thread, and as few instructions as can be: what it executes
-        // between two products is time in which the tensor core runs dry.
+        // One thread, and as few instructions as can be, each once: the tensor
+        // core's queue is a product or two long, so what this thread executes (and
+        // fetches) between two products is time in which the core stands still.
         if (warp == kSoftWarps && n > 0 && elect_one()) {
             const bool bf = std::is_same<T, __nv_bfloat16>::value;
             const uint32_t word_s = product_word(kTile, kTile, bf, false, a.negative);
-            const uint32_t word_o = product_word(kTile, 64 * a.value_blocks, bf, true, false), word_h = product_word(kTile, 64, bf, true, false);
-            const uint32_t ring_k = operand_low(ring, 16), ring_v = operand_low(ring, kSlotBytes);
-            const uint32_t q_low[2] = {operand_low(q_at, 16), operand_low(q_at + 3 * kSlotBytes, 16)};
-            const uint32_t s_bar[2] = {smem_addr(&bars->s_ready[0]), smem_addr(&bars->s_ready[1])};
-            auto scores = [&](int t, int i, bool last) {  // S_t = Q_t K_i^T
-                int slot = i * per_tile;
-                uint32_t q = q_low[t];
-                for (int c = 0; c < qk_blocks; ++c, ++slot, q += kSlotBytes >> 4) {
-                    const uint32_t k = ring_k + (slot % kSlots) * (kSlotBytes >> 4);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        product_ss<kHigh, kHigh>(tmem + kColS + t * kTile, q + 2 * e, k + 2 * e, word_s, c + e > 0);
-                }
-                product_commit(s_bar[t]);
-                if (last) product_commit(smem_addr(&bars->k_empty[i % kInFlight]));
-            };
-            auto weighted = [&](int t, int i, bool last) {  // O_t += P_t V_i
-                const int slot = (i * per_tile + qk_blocks) % kSlots;
-                const uint32_t v = ring_v + slot * (kSlotBytes >> 4), o = tmem + kColO + t * kTile, p = tmem + kColS + t * kTile;
+            const uint32_t word_o = product_word(kTile, 64 * a.value_blocks, bf, true, false);
+            const uint32_t ring_k = operand_low(ring, 16), ring_v = operand_low(ring, kSlotBytes), q_0 = operand_low(q_at, 16);
+            const uint32_t bar = smem_addr(bars);
+            const uint32_t s_0 = tmem + kColS, o_0 = tmem + kColO;
+            auto weighted = [&](int t, int slot, bool add) {  // O_t += P_t V, V's blocks from `slot` on
+                const uint32_t v = ring_v + slot * (kSlotBytes >> 4), p_at = s_0 + t * kTile, o_at = o_0 + t * kTile;
                 if (a.value_blocks == 2 && slot == kSlots - 1) {
                     // the two halves of V are not neighbours in the ring: one product each
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) product_ts<kHigh>(o, p + 8 * e, v + 128 * e, word_h, i + e > 0);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) product_ts<kHigh>(o + 64, p + 8 * e, ring_v + 128 * e, word_h, i + e > 0);
+                    const uint32_t word = product_word(kTile, 64, bf, true, false);
+#pragma unroll 1
+                    for (int e = 0; e < 8; ++e) {
+                        product_ts<kHigh>(o_at, p_at + 8 * e, v + 128 * e, word, add || e > 0);
+                        product_ts<kHigh>(o_at + 64, p_at + 8 * e, ring_v + 128 * e, word, add || e > 0);
+                    }
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) product_ts<kHigh>(o, p + 8 * e, v + 128 * e, word_o, i + e > 0);
+                    for (int e = 0; e < 8; ++e) product_ts<kHigh>(o_at, p_at + 8 * e, v + 128 * e, word_o, add || e > 0);
                 }
-                if (last) product_commit(smem_addr(&bars->v_empty[i % kInFlight]));
             };
-            bar_wait(smem_addr(&bars->q_full), 0, dead);
-            bar_wait(smem_addr(&bars->k_full[0]), 0, dead);
-            if (n0 > 0) scores(0, 0, n1 == 0);
-            if (n1 > 0) scores(1, 0, true);
-            for (int i = 0; i < n; ++i) {
-                if (cut && i == n - 1) bar_wait(smem_addr(&bars->v_clean), 0, dead);
-                else bar_wait(smem_addr(&bars->v_full[i % kInFlight]), (i / kInFlight) & 1, dead);
-                const bool more = i + 1 < n;
-                if (i < n0) {
-                    bar_wait(smem_addr(&bars->p_ready[0]), (uint32_t)i & 1, dead);
-                    tmem_after_sync();
-                    weighted(0, i, i >= n1);
-                    if (i + 1 == n0) product_commit(smem_addr(&bars->o_ready[0]));
+            auto scores = [&](int t, int slot) {  // S_t = Q_t K^T, K's blocks from `slot` on
+                uint32_t q = q_0 + t * (3 * kSlotBytes >> 4);
+#pragma unroll 1
+                for (int c = 0; c < qk_blocks; ++c, q += kSlotBytes >> 4) {
+                    const uint32_t k = ring_k + ((slot + c) & 7) * (kSlotBytes >> 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) product_ss<kHigh, kHigh>(s_0 + t * kTile, q + 2 * e, k + 2 * e, word_s, c + e > 0);
                 }
-                if (more) bar_wait(smem_addr(&bars->k_full[(i + 1) % kInFlight]), ((i + 1) / kInFlight) & 1, dead);
-                if (i + 1 < n0) scores(0, i + 1, i + 1 >= n1);
-                if (i < n1) {
-                    bar_wait(smem_addr(&bars->p_ready[1]), (uint32_t)i & 1, dead);
-                    tmem_after_sync();
-                    weighted(1, i, true);
-                    if (i + 1 == n1) product_commit(smem_addr(&bars->o_ready[1]));
-                    else scores(1, i + 1, true);
-                }
+                product_commit(bar + offsetof(Barriers, s_ready) + t * 8);
+            };
+            auto wait_k = [&](int i) { bar_wait(bar + offsetof(Barriers, k_full) + (i & 3) * 8, (i >> 2) & 1, dead); };
+            auto wait_v = [&](int i) {
+                if (cut && i == n - 1) bar_wait(bar + offsetof(Barriers, v_clean), 0, dead);
+                else bar_wait(bar + offsetof(Barriers, v_full) + (i & 3) * 8, (i >> 2) & 1, dead);
+            };
+            auto wait_p = [&](int t, int i) {
+                bar_wait(bar + offsetof(Barriers, p_ready) + t * 8, i & 1, dead);
+                tmem_after_sync();
+            };
+            auto free_k = [&](int i) { product_commit(bar + offsetof(Barriers, k_empty) + (i & 3) * 8); };
+            auto free_v = [&](int i) { product_commit(bar + offsetof(Barriers, v_empty) + (i & 3) * 8); };
+
+            bar_wait(bar + offsetof(Barriers, q_full), 0, dead);
+            wait_k(0);
+            if (n0 > 0) scores(0, 0);
+            if (n1 > 0) scores(1, 0);
+            wait_v(0);
+            int v_slot = qk_blocks & 7, k_slot = per_tile & 7;  // of V of tile i, of K of tile i + 1
+            int i = 0;
+            // While both tiles go on.  What is not urgent (slots given back, the wait
+            // for the next V) comes where the core has products queued.
+            for (; i + 1 < min(n0, n1); ++i) {
+                wait_p(0, i);
+                weighted(0, v_slot, i > 0);
+                free_k(i);
+                wait_k(i + 1);
+                scores(0, k_slot);
+                wait_p(1, i);
+                weighted(1, v_slot, i > 0);
+                free_v(i);
+                wait_v(i + 1);
+                scores(1, k_slot);
+                v_slot = (v_slot + per_tile) & 7, k_slot = (k_slot + per_tile) & 7;
             }
+            // Tiles that only some rows see.
+#pragma unroll 1
+            for (; i < n; ++i) {
+                free_k(i);
+                if (i + 1 < n) wait_k(i + 1);
+#pragma unroll 1
+                for (int t = 0; t < 2; ++t) {
+                    const int nt = t ? n1 : n0;
+                    if (i >= nt) continue;
+                    wait_p(t, i);
+                    weighted(t, v_slot, i > 0);
+                    if (i + 1 == nt) product_commit(bar + offsetof(Barriers, o_ready) + t * 8);
+                    else scores(t, k_slot);
+                }
+                free_v(i);
+                if (i + 1 < n) wait_v(i + 1);
+                v_slot = (v_slot + per_tile) & 7, k_slot = (k_slot + per_tile) & 7;
+            }
+            bar_wait(bar + offsetof(Barriers, v_empty) + ((n - 1) & 3) * 8, ((n - 1) >> 2) & 1, dead);  // every arrival has come
         }
     } else {
         registers_up<kSoftRegs>();
         // ------------------------------------------------- weights and sums
-        const int t = warp / 4, row = row0 + t * kTile + (warp % 4) * 32 + lane;
+        const int t = warp / 4, row = (t ? start1 : start0) + (warp % 4) * 32 + lane;
         const int nt = t ? n1 : n0;
         const int sees = a.causal ? min(nk, row + nk - nq + 1) : nk;  // keys [0, sees) of this row
         const int first_sees = a.causal ? min(nk, row - lane + nk - nq + 1) : nk;  // of the warp's first row: the fewest
@@ -327,7 +355,7 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
 }
 
 template <typename T>
-int run(const sim_op_latent_prefill_t *a, const Args &k, const CUtensorMap *m, unsigned grid, cudaStream_t st) {
+int run(const Args &k, const CUtensorMap *m, unsigned grid, cudaStream_t st) {
     static std::atomic<uint64_t> told;
     if (!allow_shared((const void *)k_prefill<T>, kShared, told)) return SIM_ERR_CUDA;
     k_prefill<T><<<grid, kThreads, kShared, st>>>(k, m[0], m[1], m[2], m[3], m[4]);
@@ -381,7 +409,8 @@ extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *str
     // Heads side by side: as many as keep their keys and values within about a third of L2.
     const int64_t head_bytes = a->k_rows * (a->head_dim + a->value_dim) * 2;
     const int64_t fit = head_bytes > 0 ? (40 << 20) / head_bytes : a->heads;
-    k.group = (int)(fit < 1 ? 1 : fit > a->heads ? a->heads : fit);
+    const int64_t groups = fit < 1 ? a->heads : (a->heads + fit - 1) / fit;
+    k.group = (int)((a->heads + groups - 1) / groups);  // of equal size: a last group of few heads would leave a long tail
     const int64_t grid = (int64_t)a->requests * k.row_blocks * a->heads;
     if (grid > INT32_MAX) return fail(SIM_ERR_ARG, "requests * heads * longest is too large");
 
@@ -408,5 +437,5 @@ extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *str
     }
     if (!ok) return SIM_ERR_CUDA;
     const cudaStream_t st = (cudaStream_t)stream;
-    return bf ? run<__nv_bfloat16>(a, k, m, (unsigned)grid, st) : run<__half>(a, k, m, (unsigned)grid, st);
+    return bf ? run<__nv_bfloat16>(k, m, (unsigned)grid, st) : run<__half>(k, m, (unsigned)grid, st);
 }

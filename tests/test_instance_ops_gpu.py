@@ -376,7 +376,9 @@ def check_prefill(q, key, shared, value, q_offsets, k_offsets, scale, out, lse, 
     ([1], [1], 1, 128, 64, 128), ([1, 1, 1], [1, 2, 300], 2, 128, 64, 128), ([127, 128, 129], [127, 128, 129], 2, 128, 64, 128),
     ([255, 0, 257, 1], [255, 0, 257, 1], 1, 128, 64, 128), ([64, 10], [500, 10], 3, 128, 64, 128), ([300], [300], 4, 64, 32, 64),
     ([50, 3, 77], [20, 3, 76], 2, 128, 64, 128), ([40, 5], [0, 5], 1, 128, 64, 128), ([33], [99], 5, 8, 8, 8), ([130], [700], 1, 72, 40, 104),
-    ([20], [150], 2, 128, 0, 128), ([1000], [1000], 1, 128, 64, 128), ([513], [2049], 2, 64, 64, 128)])
+    ([20], [150], 2, 128, 0, 128), ([1000], [1000], 1, 128, 64, 128), ([513], [2049], 2, 64, 64, 128),
+    ([k * 37 % 301 for k in range(40)], [k * 37 % 301 + k % 3 * 50 for k in range(40)], 12, 64, 64, 64),
+    ([600, 0, 3, 270] * 3, [1, 200, 900, 270] * 3, 40, 128, 64, 128), ([40] * 150, [40] * 150, 5, 16, 8, 24)])
 def test_prefill(nq, nk, heads, head, rot, value, dtype, causal):
     args = prefill_case(nq, nk, heads, head, rot, value, dtype, seed=sum(nq))
     scale = 1.7 / math.sqrt(head + rot)
