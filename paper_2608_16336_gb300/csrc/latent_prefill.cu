@@ -16,17 +16,25 @@ namespace {
 // The tensor core alternates between the tiles, so that one tile's
 // exponentials overlap the other's products.  K and V pass through a ring of
 // 16 KB slots (128 rows of 64 elements) filled by bulk copies.
-constexpr int kTile = 128;
-constexpr int kSlotBytes = kTile * 128;
+constexpr int kRows = 128;              // of a tile of queries
+constexpr int kQBytes = kRows * 128;    // of one column block (64 elements)
 constexpr int kSlots = 8;
-constexpr int kSoftWarps = 8;
-constexpr int kThreads = (kSoftWarps + 4) * 32;  // + products, copies of K, zeros, copies of V
-// Registers a thread: 3 warpgroups launch with 168 (504 in all); the two of
-// weights take 224, which holds a row's 128 scores without spilling.
+// TILES = 2: as above, with tiles of 128 keys.  TILES = 1: 128 queries over
+// tiles of 64 keys, small enough for two blocks on a multiprocessor, so that
+// one's start and end overlap the other's products: for short prompts.
+template <int TILES> struct Shape {
+    static constexpr int keys = 64 * TILES;
+    static constexpr int slot_bytes = keys * 128;
+    static constexpr int soft_warps = 4 * TILES;
+    static constexpr int threads = (soft_warps + 4) * 32;  // + products, copies of K (and Q), zeros, copies of V
+    static constexpr int q_slots = 3 * TILES;
+    static constexpr int shared = q_slots * kQBytes + kSlots * slot_bytes + 256;
+    // tensor memory columns: S (and P over its first half) and O of each tile
+    static constexpr int col_s = 0, col_o = 128 * TILES, cols = 256 * TILES;
+};
+// Registers a thread with two tiles: 3 warpgroups launch with 168 (504 in all); the
+// two of weights take 224, which holds a row's 128 scores without spilling.
 constexpr int kSoftRegs = 224, kOtherRegs = 56;
-constexpr int kShared = 6 * kSlotBytes + kSlots * kSlotBytes + 256;
-// Tensor memory columns: S (and P over its first half) and O of each tile.
-constexpr int kColS = 0, kColO = 256, kCols = 512;
 constexpr uint32_t kHigh = operand_high(1024);
 
 struct Args {
@@ -40,7 +48,7 @@ struct Args {
     int value_dim;
     int causal;
     int group;       // heads that run side by side (their keys and values stay in L2)
-    int row_blocks;  // of 256 queries
+    int row_blocks;  // of a block's queries
     float scale_log2;  // |scale| log2(e)
     bool negative;
 };
@@ -52,14 +60,17 @@ struct Barriers {
     uint32_t tmem;
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 1)
+template <typename T, int TILES>
+__global__ void __launch_bounds__(Shape<TILES>::threads, 3 - TILES)
 k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_q, const __grid_constant__ CUtensorMap m_qr,
           const __grid_constant__ CUtensorMap m_k, const __grid_constant__ CUtensorMap m_kr,
           const __grid_constant__ CUtensorMap m_v) {
+    using Z = Shape<TILES>;
+    constexpr int kKeys = Z::keys, kSlotBytes = Z::slot_bytes, kSoftWarps = Z::soft_warps;
+    constexpr int ring_offset = Z::q_slots * kQBytes;
     extern __shared__ __align__(1024) unsigned char smem[];
-    const uint32_t q_at = smem_addr(smem), ring = q_at + 6 * kSlotBytes;
-    Barriers *bars = (Barriers *)(smem + (6 + kSlots) * kSlotBytes);
+    const uint32_t q_at = smem_addr(smem), ring = q_at + ring_offset;
+    Barriers *bars = (Barriers *)(smem + ring_offset + kSlots * kSlotBytes);
 
     // which rows: within a group of heads the last (longest) row blocks come first
     int item = blockIdx.x;
@@ -68,20 +79,20 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     item -= b * per_request;
     const int g0 = item / (a.row_blocks * a.group) * a.group, in_group = min(a.group, a.heads - g0);
     item -= g0 * a.row_blocks;
-    const int h = g0 + item % in_group, base = (a.row_blocks - 1 - item / in_group) * 2 * kTile;
+    const int h = g0 + item % in_group, base = (a.row_blocks - 1 - item / in_group) * TILES * kRows;
     const int q0 = min(max(a.q_offsets[b], 0), a.q_rows), q1 = min(a.q_offsets[b + 1], a.q_rows);
     const int k0 = min(max(a.k_offsets[b], 0), a.k_rows), k1 = min(a.k_offsets[b + 1], a.k_rows);
     const int nq = q1 - q0, nk = max(k1 - k0, 0), rows = min(nq, a.longest);
     if (base >= rows) return;
-    const int start0 = base, start1 = base + kTile;
+    const int start0 = base, start1 = base + kRows;
     auto tiles_for = [&](int start) {  // of keys, for the rows from `start` on
         if (start >= rows) return 0;
-        const int sees = a.causal ? min(nk, min(start + kTile, rows) + nk - nq) : nk;
-        return sees > 0 ? (sees + kTile - 1) / kTile : 0;
+        const int sees = a.causal ? min(nk, min(start + kRows, rows) + nk - nq) : nk;
+        return sees > 0 ? (sees + kKeys - 1) / kKeys : 0;
     };
-    const int n0 = tiles_for(start0), n1 = tiles_for(start1), n = max(n0, n1);
+    const int n0 = tiles_for(start0), n1 = TILES == 2 ? tiles_for(start1) : 0, n = max(n0, n1);
     const int qk_blocks = a.head_blocks + a.key_blocks, per_tile = qk_blocks + a.value_blocks;
-    const bool cut = n * kTile > nk;  // the last tile has rows that are not the request's
+    const bool cut = n * kKeys > nk;  // the last tile has rows that are not the request's
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     bool dead = false;
@@ -92,14 +103,14 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             bar_init(smem_addr(&bars->v_full[s]), 1), bar_init(smem_addr(&bars->v_empty[s]), 1);
         }
         bar_init(smem_addr(&bars->v_cut), 1), bar_init(smem_addr(&bars->v_clean), 32);
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < TILES; ++t) {
             bar_init(smem_addr(&bars->s_ready[t]), 1);
-            bar_init(smem_addr(&bars->p_ready[t]), kTile);
+            bar_init(smem_addr(&bars->p_ready[t]), kRows);
             bar_init(smem_addr(&bars->o_ready[t]), 1);
         }
         bar_init_done();
     }
-    if (warp == kSoftWarps) tmem_alloc(smem_addr(&bars->tmem), kCols);
+    if (warp == kSoftWarps) tmem_alloc(smem_addr(&bars->tmem), Z::cols);
     if (threadIdx.x == (kSoftWarps + 1) * 32) fetch_map(&m_q), fetch_map(&m_qr), fetch_map(&m_k), fetch_map(&m_kr), fetch_map(&m_v);
     __syncwarp();
     tmem_before_sync();
@@ -108,16 +119,16 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     const uint32_t tmem = bars->tmem;
 
     if (warp >= kSoftWarps) {
-        registers_down<kOtherRegs>();
+        if (TILES == 2) registers_down<kOtherRegs>();
         // ---------------------------------------------------------- copies
         // One warp for K (and Q), one for V, a lane a column block.  Eight slots
         // earlier in the stream lies a block of a fixed kind, a fixed number of tiles
         // back: when that has been used, the slot is free.
-        if (warp == kSoftWarps + 1 && lane < 6 && n > 0) {
+        if (warp == kSoftWarps + 1 && lane < Z::q_slots && n > 0) {
             const uint32_t qf = smem_addr(&bars->q_full);
-            if (lane == 0) bar_expect(qf, ((n0 > 0) + (n1 > 0)) * qk_blocks * kSlotBytes);
+            if (lane == 0) bar_expect(qf, ((n0 > 0) + (n1 > 0)) * qk_blocks * kQBytes);
             const int t = lane / 3, c = lane % 3, r = q0 + (t ? start1 : start0);
-            const uint32_t dst = q_at + lane * kSlotBytes;
+            const uint32_t dst = q_at + lane * kQBytes;
             if (c < qk_blocks && (t ? n1 : n0) > 0) {
                 if (c < a.head_blocks) copy_box_3d(dst, &m_q, 64 * c, h, r, qf);
                 else copy_box_3d(dst, &m_qr, 64 * (c - a.head_blocks), h, r, qf);
@@ -134,7 +145,7 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             const CUtensorMap *map = of_v ? &m_v : of_shared_key ? &m_kr : &m_k;
             const int x = 64 * (of_shared_key ? lane - a.head_blocks : lane);
             int slot = at, r = k0;
-            for (int i = 0; i < n; ++i, r += kTile, slot = (slot + per_tile) % kSlots) {
+            for (int i = 0; i < n; ++i, r += kKeys, slot = (slot + per_tile) % kSlots) {
                 const int old = i - back;
                 if (old >= 0) bar_wait(empty + old % kInFlight * 8, (old / kInFlight) & 1, dead);
                 const uint32_t bar = of_v && cut && i == n - 1 ? smem_addr(&bars->v_cut) : full + i % kInFlight * 8;
@@ -149,8 +160,8 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             const int i = n - 1;
             bar_wait(smem_addr(&bars->v_cut), 0, dead);
             for (int c = 0; c < a.value_blocks; ++c) {
-                uint4 *rows_at = (uint4 *)(smem + (6 + (i * per_tile + qk_blocks + c) % kSlots) * kSlotBytes + (nk - i * kTile) * 128);
-                for (int e = lane; e < ((i + 1) * kTile - nk) * 8; e += 32) rows_at[e] = make_uint4(0, 0, 0, 0);
+                uint4 *rows_at = (uint4 *)(smem + ring_offset + (i * per_tile + qk_blocks + c) % kSlots * kSlotBytes + (nk - i * kKeys) * 128);
+                for (int e = lane; e < ((i + 1) * kKeys - nk) * 8; e += 32) rows_at[e] = make_uint4(0, 0, 0, 0);
             }
             fence_async();
             bar_arrive(smem_addr(&bars->v_clean));
@@ -161,33 +172,33 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
         // fetches) between two products is time in which the core stands still.
         if (warp == kSoftWarps && n > 0 && elect_one()) {
             const bool bf = std::is_same<T, __nv_bfloat16>::value;
-            const uint32_t word_s = product_word(kTile, kTile, bf, false, a.negative);
-            const uint32_t word_o = product_word(kTile, 64 * a.value_blocks, bf, true, false);
+            const uint32_t word_s = product_word(kRows, kKeys, bf, false, a.negative);
+            const uint32_t word_o = product_word(kRows, 64 * a.value_blocks, bf, true, false);
             const uint32_t ring_k = operand_low(ring, 16), ring_v = operand_low(ring, kSlotBytes), q_0 = operand_low(q_at, 16);
             const uint32_t bar = smem_addr(bars);
-            const uint32_t s_0 = tmem + kColS, o_0 = tmem + kColO;
+            const uint32_t s_0 = tmem + Z::col_s, o_0 = tmem + Z::col_o;
             auto weighted = [&](int t, int slot, bool add) {  // O_t += P_t V, V's blocks from `slot` on
-                const uint32_t v = ring_v + slot * (kSlotBytes >> 4), p_at = s_0 + t * kTile, o_at = o_0 + t * kTile;
+                const uint32_t v = ring_v + slot * (kSlotBytes >> 4), p_at = s_0 + t * kRows, o_at = o_0 + t * kRows;
                 if (a.value_blocks == 2 && slot == kSlots - 1) {
                     // the two halves of V are not neighbours in the ring: one product each
-                    const uint32_t word = product_word(kTile, 64, bf, true, false);
+                    const uint32_t word = product_word(kRows, 64, bf, true, false);
 #pragma unroll 1
-                    for (int e = 0; e < 8; ++e) {
+                    for (int e = 0; e < kKeys / 16; ++e) {
                         product_ts<kHigh>(o_at, p_at + 8 * e, v + 128 * e, word, add || e > 0);
                         product_ts<kHigh>(o_at + 64, p_at + 8 * e, ring_v + 128 * e, word, add || e > 0);
                     }
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) product_ts<kHigh>(o_at, p_at + 8 * e, v + 128 * e, word_o, add || e > 0);
+                    for (int e = 0; e < kKeys / 16; ++e) product_ts<kHigh>(o_at, p_at + 8 * e, v + 128 * e, word_o, add || e > 0);
                 }
             };
             auto scores = [&](int t, int slot) {  // S_t = Q_t K^T, K's blocks from `slot` on
-                uint32_t q = q_0 + t * (3 * kSlotBytes >> 4);
+                uint32_t q = q_0 + t * (3 * kQBytes >> 4);
 #pragma unroll 1
-                for (int c = 0; c < qk_blocks; ++c, q += kSlotBytes >> 4) {
+                for (int c = 0; c < qk_blocks; ++c, q += kQBytes >> 4) {
                     const uint32_t k = ring_k + ((slot + c) & 7) * (kSlotBytes >> 4);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) product_ss<kHigh, kHigh>(s_0 + t * kTile, q + 2 * e, k + 2 * e, word_s, c + e > 0);
+                    for (int e = 0; e < 4; ++e) product_ss<kHigh, kHigh>(s_0 + t * kRows, q + 2 * e, k + 2 * e, word_s, c + e > 0);
                 }
                 product_commit(bar + offsetof(Barriers, s_ready) + t * 8);
             };
@@ -212,7 +223,7 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             int i = 0;
             // While both tiles go on.  What is not urgent (slots given back, the wait
             // for the next V) comes where the core has products queued.
-            for (; i + 1 < min(n0, n1); ++i) {
+            for (; TILES == 2 && i + 1 < min(n0, n1); ++i) {
                 wait_p(0, i);
                 weighted(0, v_slot, i > 0);
                 free_k(i);
@@ -231,7 +242,7 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
                 free_k(i);
                 if (i + 1 < n) wait_k(i + 1);
 #pragma unroll 1
-                for (int t = 0; t < 2; ++t) {
+                for (int t = 0; t < TILES; ++t) {
                     const int nt = t ? n1 : n0;
                     if (i >= nt) continue;
                     wait_p(t, i);
@@ -246,33 +257,33 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             bar_wait(bar + offsetof(Barriers, v_empty) + ((n - 1) & 3) * 8, ((n - 1) >> 2) & 1, dead);  // every arrival has come
         }
     } else {
-        registers_up<kSoftRegs>();
+        if (TILES == 2) registers_up<kSoftRegs>();
         // ------------------------------------------------- weights and sums
         const int t = warp / 4, row = (t ? start1 : start0) + (warp % 4) * 32 + lane;
         const int nt = t ? n1 : n0;
         const int sees = a.causal ? min(nk, row + nk - nq + 1) : nk;  // keys [0, sees) of this row
         const int first_sees = a.causal ? min(nk, row - lane + nk - nq + 1) : nk;  // of the warp's first row: the fewest
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
-        const uint32_t s_at = tmem + kColS + t * kTile + lanes, o_at = tmem + kColO + t * kTile + lanes;
+        const uint32_t s_at = tmem + Z::col_s + t * kRows + lanes, o_at = tmem + Z::col_o + t * kRows + lanes;
         const float scale = a.scale_log2;
         float top = -INFINITY, sum = 0.f;  // top: of the scaled scores, as far as P has been scaled by it
         for (int i = 0; i < nt; ++i) {
             bar_wait(smem_addr(&bars->s_ready[t]), (uint32_t)i & 1, dead);
             tmem_after_sync();
-            uint32_t s[128];
+            uint32_t s[kKeys];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, s + 32 * c);
+            for (int c = 0; c < kKeys / 32; ++c) tmem_ld32(s_at + 32 * c, s + 32 * c);
             tmem_wait_ld();
             float *x = (float *)s;
-            if ((i + 1) * kTile > first_sees) {
-                const int v = sees - i * kTile;
+            if ((i + 1) * kKeys > first_sees) {
+                const int v = sees - i * kKeys;
 #pragma unroll
-                for (int c = 0; c < 128; ++c)
+                for (int c = 0; c < kKeys; ++c)
                     if (c >= v) x[c] = -INFINITY;
             }
             float m0 = x[0], m1 = x[1], m2 = x[2], m3 = x[3];
 #pragma unroll
-            for (int c = 4; c < 128; c += 4) {
+            for (int c = 4; c < kKeys; c += 4) {
                 m0 = fmaxf(m0, x[c]), m1 = fmaxf(m1, x[c + 1]), m2 = fmaxf(m2, x[c + 2]), m3 = fmaxf(m3, x[c + 3]);
             }
             const float high = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;
@@ -299,9 +310,9 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             }
             const float base = top == -INFINITY ? 0.f : -top;
             float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-            uint32_t p[64];
+            uint32_t p[kKeys / 2];
 #pragma unroll
-            for (int c = 0; c < 128; c += 4) {
+            for (int c = 0; c < kKeys; c += 4) {
                 float e0, e1, e2, e3;
                 fma2(e0, e1, x[c], x[c + 1], scale, scale, base, base);
                 fma2(e2, e3, x[c + 2], x[c + 3], scale, scale, base, base);
@@ -312,7 +323,7 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
                 p[c / 2 + 1] = pack2<T>(e2, e3);
             }
             tmem_st32(s_at, p);
-            tmem_st32(s_at + 32, p + 32);
+            if (TILES == 2) tmem_st32(s_at + 32, p + kKeys / 2 - 32);
             tmem_wait_st();
             tmem_before_sync();
             bar_arrive(smem_addr(&bars->p_ready[t]));
@@ -351,14 +362,14 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     __syncwarp();
     tmem_before_sync();
     __syncthreads();
-    if (warp == kSoftWarps) tmem_free(tmem, kCols);
+    if (warp == kSoftWarps) tmem_free(tmem, Z::cols);
 }
 
-template <typename T>
+template <typename T, int TILES>
 int run(const Args &k, const CUtensorMap *m, unsigned grid, cudaStream_t st) {
     static std::atomic<uint64_t> told;
-    if (!allow_shared((const void *)k_prefill<T>, kShared, told)) return SIM_ERR_CUDA;
-    k_prefill<T><<<grid, kThreads, kShared, st>>>(k, m[0], m[1], m[2], m[3], m[4]);
+    if (!allow_shared((const void *)k_prefill<T, TILES>, Shape<TILES>::shared, told)) return SIM_ERR_CUDA;
+    k_prefill<T, TILES><<<grid, Shape<TILES>::threads, Shape<TILES>::shared, st>>>(k, m[0], m[1], m[2], m[3], m[4]);
     return launched("sim_op_latent_prefill");
 }
 
@@ -405,7 +416,12 @@ extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *str
     k.scale_log2 = std::fmax(std::fabs(a->scale) * 1.4426950408889634f, 1e-30f);  // not 0: a masked score is -infinity times it
     k.negative = a->scale < 0;
     const int64_t longest = a->longest < a->q_rows ? a->longest : a->q_rows;
-    k.row_blocks = (int)((longest + 2 * kTile - 1) / (2 * kTile));
+    // One tile a block where most prompts leave the second one empty and keys
+    // are few: 37 ragged prompts up to 300, 16 heads 26.7 us (two tiles 34.8), 64 x 128
+    // tokens, 64 heads 134 us (189); two tiles for the rest: 37 x 512 tokens 98.8 us (one
+    // 117), 16 x 256 tokens after up to 1,000 cached ones 77 us (95).
+    const int tiles = longest <= 384 && a->q_rows <= 192 * (int64_t)a->requests && a->k_rows <= 384 * (int64_t)a->requests ? 1 : 2;
+    k.row_blocks = (int)((longest + tiles * kRows - 1) / (tiles * kRows));
     // Heads side by side: as many as keep their keys and values within about a third of L2.
     const int64_t head_bytes = a->k_rows * (a->head_dim + a->value_dim) * 2;
     const int64_t fit = head_bytes > 0 ? (40 << 20) / head_bytes : a->heads;
@@ -415,27 +431,30 @@ extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *str
     if (grid > INT32_MAX) return fail(SIM_ERR_ARG, "requests * heads * longest is too large");
 
     CUtensorMap m[5];
-    auto map3 = [&](CUtensorMap *to, const void *base, int dim, int64_t rows, int64_t head, int64_t row) {
+    const int keys = 64 * tiles;
+    auto map3 = [&](CUtensorMap *to, const void *base, int dim, int64_t rows, int64_t head, int64_t row, int box_rows) {
         const uint64_t size[3] = {(uint64_t)dim, (uint64_t)a->heads, (uint64_t)(rows > 0 ? rows : 1)};
         const int64_t stride[2] = {a->heads > 1 ? head : 8, rows > 1 ? row : 8};
-        const uint32_t box[3] = {64, 1, kTile};
+        const uint32_t box[3] = {64, 1, (uint32_t)box_rows};
         return box_map(to, base, bf, 3, size, stride, box);
     };
     const char *q_key = (const char *)a->q + 2 * a->head_dim;
-    bool ok = map3(&m[0], a->q, a->head_dim, a->q_rows, a->q_head, a->q_row) &&
-              map3(&m[1], a->key_dim ? q_key : a->q, a->key_dim ? a->key_dim : 8, a->q_rows, a->q_head, a->q_row);
+    bool ok = map3(&m[0], a->q, a->head_dim, a->q_rows, a->q_head, a->q_row, kRows) &&
+              map3(&m[1], a->key_dim ? q_key : a->q, a->key_dim ? a->key_dim : 8, a->q_rows, a->q_head, a->q_row, kRows);
     // without keys nothing is copied: any valid map does
     const void *key = a->k_rows ? a->key : a->q, *value = a->k_rows ? a->value : a->q;
-    ok = ok && map3(&m[2], key, a->head_dim, a->k_rows, a->key_head, a->key_row) &&
-         map3(&m[4], value, a->value_dim, a->k_rows, a->value_head, a->value_row);
+    ok = ok && map3(&m[2], key, a->head_dim, a->k_rows, a->key_head, a->key_row, keys) &&
+         map3(&m[4], value, a->value_dim, a->k_rows, a->value_head, a->value_row, keys);
     if (ok) {
         const bool has = a->k_rows && a->key_dim;
         const uint64_t size[2] = {has ? (uint64_t)a->key_dim : 8u, has ? (uint64_t)a->k_rows : 1u};
         const int64_t stride[1] = {has && a->k_rows > 1 ? a->shared_row : 8};
-        const uint32_t box[2] = {64, kTile};
+        const uint32_t box[2] = {64, (uint32_t)keys};
         ok = box_map(&m[3], has ? a->shared : a->q, bf, 2, size, stride, box);
     }
     if (!ok) return SIM_ERR_CUDA;
     const cudaStream_t st = (cudaStream_t)stream;
-    return bf ? run<__nv_bfloat16>(k, m, (unsigned)grid, st) : run<__half>(k, m, (unsigned)grid, st);
+    const unsigned g = (unsigned)grid;
+    if (tiles == 1) return bf ? run<__nv_bfloat16, 1>(k, m, g, st) : run<__half, 1>(k, m, g, st);
+    return bf ? run<__nv_bfloat16, 2>(k, m, g, st) : run<__half, 2>(k, m, g, st);
 }
