@@ -21,6 +21,7 @@ constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kCoarse = 4096;  // bins of the first, approximate histogram
 constexpr int kFine = 256;     // bins of an exact one
 constexpr int kList = 1024;    // candidates for a threshold
+constexpr int kFew = 128;      // so few that each is compared with all
 constexpr int kBinsEach = kCoarse / kThreads;
 constexpr float kUnit = 1099511627776.f, kUnitLog2 = 40.f;
 constexpr int kMostCluster = 8;
@@ -39,18 +40,22 @@ __device__ __forceinline__ float exp2_near(float x) {
     return y;
 }
 
-// A sum of weights.  A weight x <= 2^40 is cut into x = 2^18 hi + lo by
-// additions of 2^23 (whose sums' low bits are the whole number), because
-// conversions to 64 bits run at a fraction of the rate; the constant in the words
-// is taken out at the end.  32 bits hold 1,024 of each.
+// A weight x <= 2^40 cut into x = 2^18 hi + lo by additions of 2^23 (whose
+// sums' low bits are the whole number), because conversions to 64 bits run at a
+// fraction of the rate.  The sums keep the constant, which is taken out at the end; 32
+// bits hold 1,023 of each.
+struct Cut {
+    uint32_t hi, lo;
+    __device__ __forceinline__ explicit Cut(float x) {
+        const float t = __fadd_rz(x * 3.814697265625e-06f, 8388608.f);
+        hi = __float_as_uint(t), lo = __float_as_uint(fmaf(t - 8388608.f, -262144.f, x) + 8388608.f);
+    }
+    __device__ __forceinline__ u64 units() const { return ((u64)(hi - 0x4B000000u) << 18) + (lo - 0x4B000000u); }
+};
 struct Mass {
     uint32_t hi = 0, lo = 0, n = 0;
-    __device__ __forceinline__ void add(float x) {
-        const float t = __fadd_rz(x * 3.814697265625e-06f, 8388608.f);
-        const float rest = fmaf(t - 8388608.f, -262144.f, x) + 8388608.f;
-        hi += __float_as_uint(t), lo += __float_as_uint(rest), ++n;
-    }
-    __device__ __forceinline__ void add_if(bool yes, float x) { add(yes ? x : 0.f); }
+    __device__ __forceinline__ void add(const Cut &c) { hi += c.hi, lo += c.lo, ++n; }
+    __device__ __forceinline__ void add_if(bool yes, const Cut &c) { hi += yes ? c.hi : 0, lo += yes ? c.lo : 0, n += yes; }
     __device__ __forceinline__ u64 units() const { return ((u64)(hi - n * 0x4B000000u) << 18) + (lo - n * 0x4B000000u); }
 };
 
@@ -70,16 +75,8 @@ __device__ __forceinline__ u64 share_of(u64 x, float f, bool up) {
 
 struct Weights {
     float top, per;  // the largest logit, log2(e) / temperature
-    // in units; without a finite top the +infinite logits share it all
-    __device__ __forceinline__ float of(float v) const {
-        if (top == INFINITY) return v == INFINITY ? kUnit : 0.f;
-        return exp2_near(fminf((v - top) * per, 0.f) + kUnitLog2);
-    }
-    __device__ __forceinline__ u64 units(float v) const {
-        Mass m;
-        m.add(of(v));
-        return m.units();
-    }
+    __device__ __forceinline__ float of(float v) const { return exp2_near(fmaf(v - top, per, kUnitLog2)); }  // in units
+    __device__ __forceinline__ u64 units(float v) const { return Cut(of(v)).units(); }
 };
 
 struct Sums {
@@ -128,6 +125,11 @@ template <typename T> struct Part {
     const T *row;    // the row's first logit, `skip` elements after a 16-byte boundary
     const T *held;   // the part in shared memory, or NULL
     int skip, vocab, begin, warp_len;  // positions count from that boundary
+    bool endless;    // the largest logit is +infinity: it counts as 0, all others as -infinity
+    __device__ __forceinline__ float value(T x) const {
+        const float v = fmaxf(elem<T>::to(x), -INFINITY);  // NaN: -infinity
+        return !endless ? v : v == INFINITY ? 0.f : -INFINITY;
+    }
 
     // 16 bytes of the part from position p on (relative to it), -infinity where the row is not
     __device__ __forceinline__ void global(int p, T *x) const {
@@ -139,22 +141,26 @@ template <typename T> struct Part {
             for (int e = 0; e < N; ++e) x[e] = i + e >= 0 && i + e < vocab ? row[i + e] : elem<T>::from(-INFINITY);
         }
     }
+    // The N logits at position p of the part.
+    __device__ __forceinline__ void at(int p, float *v) const {
+        alignas(16) T x[N];
+        if (held) *(uint4 *)x = *(const uint4 *)(held + p);
+        else global(p, x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = value(x[e]);
+    }
     // f(position, logits) over this warp's stretch, in vocabulary order: lane by lane within a step
     template <typename F> __device__ __forceinline__ void each(F f) const {
-        const int lane = threadIdx.x % 32, at = threadIdx.x / 32 * warp_len;
-        for (int p = at + lane * N; p < at + warp_len; p += 32 * N) {
-            alignas(16) T x[N];
-            if (held) *(uint4 *)x = *(const uint4 *)(held + p);
-            else global(p, x);
+        const int lane = threadIdx.x % 32, from = threadIdx.x / 32 * warp_len;
+        for (int p = from + lane * N; p < from + warp_len; p += 32 * N) {
             float v[N];
-#pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = fmaxf(elem<T>::to(x[e]), -INFINITY);  // NaN: -infinity
+            at(p, v);
             f(p, v);
         }
     }
 };
 
-template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ sim_op_sample_t a, int warp_len, bool staged) {
+template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ sim_op_sample_t a, int warp_len, bool staged, int bins) {
     extern __shared__ __align__(16) unsigned char dynamic[];
     __shared__ Shared sh;
     cg::cluster_group cluster = cg::this_cluster();
@@ -170,7 +176,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
     part.vocab = a.vocab;
     part.warp_len = warp_len;
     part.begin = rank * warp_len * kWarps;
-    part.held = nullptr;
+    part.held = nullptr, part.endless = false;
     T *const mine = (T *)dynamic;
 
     int turn = 0;  // which of the two exchange buffers
@@ -181,7 +187,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
     auto peer = [&](auto *p, int r) { return blocks > 1 ? cluster.map_shared_rank(p, r) : p; };
 
     // ------------------------------------------------ the row, its largest logit
-    uint32_t best = 0;
+    float high = -INFINITY;
     {
         const int at = warp * warp_len;
         for (int p = at + lane * Part<T>::N; p < at + warp_len; p += 32 * Part<T>::N) {
@@ -189,26 +195,27 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
             part.global(p, x);
             if (staged) *(uint4 *)(mine + p) = *(const uint4 *)x;
 #pragma unroll
-            for (int e = 0; e < Part<T>::N; ++e) best = max(best, key_of(fmaxf(elem<T>::to(x[e]), -INFINITY)));
+            for (int e = 0; e < Part<T>::N; ++e) high = fmaxf(high, elem<T>::to(x[e]));
         }
         if (staged) part.held = mine;
     }
-    for (int b = threadIdx.x; b < kCoarse; b += kThreads) sh.coarse[b] = 0;
+    for (int b = threadIdx.x; b < bins; b += kThreads) sh.coarse[b] = 0;
     if (threadIdx.x < 2) sh.listed[threadIdx.x] = 0;
-    best = __reduce_max_sync(~0u, best);
+    uint32_t best = __reduce_max_sync(~0u, key_of(high));
     if (lane == 0) sh.warp_count[warp] = best;
     __syncthreads();
     best = __reduce_max_sync(~0u, sh.warp_count[lane % kWarps]);
     if (threadIdx.x == 0) sh.sums[turn].high = best;
     barrier();
-    for (int r = 0; r < blocks; ++r) best = max(best, peer(&sh.sums[turn].high, r)[0]);
+    best = __reduce_max_sync(~0u, *peer(&sh.sums[turn].high, lane % blocks));
     turn ^= 1;
 
     Weights w;
     w.top = value_of(best);
+    if (w.top == INFINITY) part.endless = true, w.top = 0.f, best = key_of(0.f);
     const float t = a.temperature ? a.temperature[row] : 1.f;
     const bool greedy = !(t > 0);
-    w.per = fmaxf(1.4426950408889634f / t, 1.2e-38f);  // not 0, which would take -infinity to NaN
+    w.per = fminf(fmaxf(1.4426950408889634f / t, 1.2e-38f), 3e38f);  // not 0 or infinite: -infinity * 0 and 0 * infinity are NaN
     const int k = a.top_k ? a.top_k[row] : 0;
     const float p = a.top_p ? a.top_p[row] : 1.f;
     // min_p in units; the largest logit always stays
@@ -227,11 +234,15 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
             if (lane == 0) sh.sums[turn].mass = m, sh.sums[turn].mass2 = m2, sh.sums[turn].count = c;
         }
         barrier();
-        out.mass = 0, out.mass2 = 0, out.count = 0;
-        for (int r = 0; r < blocks; ++r) {
-            const Sums *s = peer(&sh.sums[turn], r);
-            if (before && r == rank) *before = out;
-            out.mass += s->mass, out.mass2 += s->mass2, out.count += s->count;
+        // a lane a block
+        const Sums *from = peer(&sh.sums[turn], lane % blocks);
+        const bool real = lane < blocks;
+        const u64 m = real ? from->mass : 0, m2 = real ? from->mass2 : 0;
+        const uint32_t c = real ? from->count : 0;
+        out.mass = warp_total(m), out.mass2 = warp_total(m2), out.count = __reduce_add_sync(~0u, c);
+        if (before) {
+            before->mass = warp_total(lane < rank ? m : 0);
+            before->count = __reduce_add_sync(~0u, lane < rank ? c : 0);
         }
         turn ^= 1;
     };
@@ -251,30 +262,37 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
 
     if (limit_k || limit_p) {
         // ------------------------------ where to look: counts over 41 powers of two of weight
-        const float fine = (float)(kCoarse - 1) / 41.f, slope = w.per * fine;
+        const float fine = (bins - 1) / 41.f, slope = fminf(w.per * fine, 3e38f), last_bin = (float)(bins - 1);
         part.each([&](int, const float *v) {
 #pragma unroll
             for (int e = 0; e < Part<T>::N; ++e) {
-                const int bin = min(kCoarse - 1, max(0, __float2int_rz((w.top - v[e]) * slope)));
+                const uint32_t bin = __float_as_uint(fminf((w.top - v[e]) * slope, last_bin) + 8388608.f) & 0xFFFF;
                 if (v[e] > -INFINITY) atomicAdd(&sh.coarse[bin], 1u);
             }
         });
         barrier();
-        // a thread has some neighbouring bins; counts and approximate weight up to and with them
+        // a thread has some neighbouring bins; counts and approximate weight up to
+        // and with them.  (Every block begins with its own: all reading the same one's memory at a time takes twice as long.)
+        const int each_bins = bins / kThreads, first_bin = each_bins * threadIdx.x;
         uint32_t bin_count[kBinsEach] = {};
-        for (int r = 0; r < blocks; ++r) {
-            const uint4 *from = (const uint4 *)peer(&sh.coarse[kBinsEach * threadIdx.x], r);
+        for (int q = 0; q < blocks; ++q) {
+            const int r = rank + q < blocks ? rank + q : rank + q - blocks;
+            const uint32_t *from = peer(&sh.coarse[first_bin], r);
+            if (each_bins == 8) {
+                const uint4 c = *(const uint4 *)from, d = *(const uint4 *)(from + 4);
+                bin_count[0] += c.x, bin_count[1] += c.y, bin_count[2] += c.z, bin_count[3] += c.w;
+                bin_count[4] += d.x, bin_count[5] += d.y, bin_count[6] += d.z, bin_count[7] += d.w;
+            } else {
 #pragma unroll
-            for (int e = 0; e < kBinsEach / 4; ++e) {
-                const uint4 c = from[e];
-                bin_count[4 * e] += c.x, bin_count[4 * e + 1] += c.y, bin_count[4 * e + 2] += c.z, bin_count[4 * e + 3] += c.w;
+                for (int e = 0; e < 4; ++e)
+                    if (e < each_bins) bin_count[e] += from[e];
             }
         }
-        auto bin_weight = [&](int bin) { return exp2_near(40.f - (bin + 0.5f) / fine); };
+        auto bin_weight = [&](int bin) { return exp2_near(40.f - bin / fine); };  // bins are about their middles
         uint32_t counts = 0;
         float masses = 0.f;
 #pragma unroll
-        for (int e = 0; e < kBinsEach; ++e) counts += bin_count[e], masses += bin_count[e] * bin_weight(kBinsEach * threadIdx.x + e);
+        for (int e = 0; e < kBinsEach; ++e) counts += bin_count[e], masses += bin_count[e] * bin_weight(first_bin + e);
         uint32_t prior_count = counts;
         float prior_mass = masses;
 #pragma unroll
@@ -305,13 +323,13 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
         // spare on both sides; and the weight above it with as much of it as the count takes.
         auto look = [&](bool by_mass, uint32_t want, float want_mass, uint32_t &lo, uint32_t &hi, float &to_there) {
             __syncthreads();
-            if (threadIdx.x == 0) sh.found[0] = kCoarse;
+            if (threadIdx.x == 0) sh.found[0] = bins;
             __syncthreads();
             uint32_t c = prior_count;
             float m = prior_mass;
 #pragma unroll
             for (int e = 0; e < kBinsEach; ++e) {
-                const int bin = kBinsEach * threadIdx.x + e;
+                const int bin = first_bin + e;
                 const float bw = bin_weight(bin), m2 = m + bin_count[e] * bw;
                 const uint32_t c2 = c + bin_count[e];
                 if (by_mass ? m < want_mass && m2 >= want_mass : c < want && c2 >= want) {
@@ -321,11 +339,11 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
             }
             __syncthreads();
             const int bin = (int)sh.found[0];
-            to_there = bin < kCoarse ? sh.found_real[0] : masses;
+            to_there = bin < bins ? sh.found_real[0] : masses;
             hi = best, lo = 0;
-            if (bin < kCoarse) {
-                if (bin > 1) hi = min(best, key_of(w.top - (bin - 1) / slope));
-                if (bin < kCoarse - 2) lo = key_of(w.top - (bin + 2) / slope);
+            if (bin < bins) {
+                if (bin > 1) hi = min(best, key_of(w.top - (bin - 1.5f) / slope));
+                if (bin < bins - 2) lo = key_of(w.top - (bin + 1.5f) / slope);
                 if (lo > hi) lo = 0;
             }
         };
@@ -347,7 +365,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
                         const uint32_t key = key_of(v[e]), cell = key >> shift;
                         if (cell >= base + n) {
                             ++count;
-                            if (by_mass) mass.add(w.of(v[e]));
+                            if (by_mass) mass.add(Cut(w.of(v[e])));
                         } else if (cell >= base && v[e] > -INFINITY) {
                             atomicAdd(&sh.count[turn][cell - base], 1u);
                             if (by_mass) {
@@ -429,25 +447,29 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
         {
             Mass m1, m2;  // of all (of those above the count's candidates), of those above the weight's
             uint32_t count = 0;
+            // (comparisons of logits: a key is only made of a candidate)
+            auto floor_of = [&](uint32_t key) { return key ? value_of(key) : -INFINITY; };
+            const float top_k = limit_k ? value_of(hi_k) : 0.f, low_k = floor_of(lo_k), top_p = limit_p ? value_of(hi_p) : 0.f, low_p = floor_of(lo_p);
+            auto list = [&](int l, float v, int pos) {
+                const uint32_t at = atomicAdd(&sh.listed[l], 1u);
+                if (at < kList) sh.list[l][at] = key_of(v), sh.place[l][at] = pos;
+            };
             part.each([&](int pos, const float *v) {
 #pragma unroll
                 for (int e = 0; e < Part<T>::N; ++e) {
-                    const uint32_t key = key_of(v[e]);
-                    const float x = w.of(v[e]);
-                    m1.add_if(!limit_k || key > hi_k, x);
+                    const Cut x(w.of(v[e]));
                     if (limit_k) {
-                        count += key > hi_k;
-                        if (key <= hi_k && key >= lo_k) {
-                            const uint32_t at = atomicAdd(&sh.listed[0], 1u);
-                            if (at < kList) sh.list[0][at] = key, sh.place[0][at] = pos + e;
-                        }
+                        const bool above = v[e] > top_k;
+                        m1.add_if(above, x);
+                        count += above;
+                        if (!above && v[e] >= low_k) list(0, v[e], pos + e);
+                    } else {
+                        m1.add(x);
                     }
                     if (limit_p) {
-                        m2.add_if(key > hi_p, x);
-                        if (key <= hi_p && key >= lo_p) {
-                            const uint32_t at = atomicAdd(&sh.listed[1], 1u);
-                            if (at < kList) sh.list[1][at] = key, sh.place[1][at] = pos + e;
-                        }
+                        const bool above = v[e] > top_p;
+                        m2.add_if(above, x);
+                        if (!above && v[e] >= low_p) list(1, v[e], pos + e);
                     }
                 }
             });
@@ -461,30 +483,55 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
                 sh.warp_hi[threadIdx.x] = sh.warp_lo[threadIdx.x] = 0;
             }
         }
-        // every block takes the candidates of all
+        // every block takes the candidates of all: a warp a block's list
         int n_of[2];
+#pragma unroll
         for (int l = 0; l < 2; ++l) {
-            uint32_t n = 0;
-            for (int r = 0; r < blocks; ++r) {
-                const uint32_t c = *peer(&sh.listed[l], r);
-                if (c > kList || n + c > kList) n = kList + 1;
-                else {
-                    const uint32_t *from = peer(&sh.list[l][0], r);
-                    for (uint32_t i = threadIdx.x; i < c; i += kThreads) {
-                        const uint32_t key = from[i];
-                        sh.all.key[l][n + i] = key;
-                        if (l == limit_p) sh.all.unit[n + i] = w.units(value_of(key));
-                    }
-                    n += c;
+            const uint32_t c = lane < blocks ? *peer(&sh.listed[l], lane % blocks) : 0;
+            uint32_t end = c;
+#pragma unroll
+            for (int o = 1; o < kMostCluster; o <<= 1) {
+                const uint32_t u = __shfl_up_sync(~0u, end, o);
+                if (lane >= o) end += u;
+            }
+            const uint32_t n = __shfl_sync(~0u, end, blocks - 1);
+            n_of[l] = n <= kList ? (int)n : -1;
+            const int r = warp - l * kMostCluster;
+            if (n <= kList && r >= 0 && r < blocks) {
+                const uint32_t to = __shfl_sync(~0u, end - c, r), mine_of = __shfl_sync(~0u, c, r);
+                const uint32_t *from = peer(&sh.list[l][0], r);
+                for (uint32_t i = lane; i < mine_of; i += 32) {
+                    const uint32_t key = from[i];
+                    sh.all.key[l][to + i] = key;
+                    if (l == limit_p) sh.all.unit[to + i] = w.units(value_of(key));
                 }
             }
-            n_of[l] = n <= kList ? (int)n : -1;
         }
         __syncthreads();
         // The threshold among the candidates: each warp tries a key at a time.  False if it is not among them (the bins are approximate) or they are too many.
         auto among = [&](bool by_mass, u64 want, u64 above, uint32_t lo, uint32_t hi, u64 &before, uint32_t &at, uint32_t &same) -> bool {
             const int l = by_mass, n = n_of[l];
             if (n < 0 || above >= want) return false;
+            if (n <= kFew) {  // each candidate against all
+                __syncthreads();
+                if (threadIdx.x == 0) sh.found[1] = 0;
+                __syncthreads();
+                if ((int)threadIdx.x < n) {
+                    const uint32_t key = sh.all.key[l][threadIdx.x];
+                    u64 over = above;
+                    uint32_t eq = 0;
+                    for (int j = 0; j < n; ++j) {
+                        const uint32_t other = sh.all.key[l][j];
+                        if (other > key) over += by_mass ? sh.all.unit[j] : 1;
+                        eq += other == key;
+                    }
+                    const u64 each = by_mass ? sh.all.unit[threadIdx.x] : 1;
+                    if (over < want && over + eq * each >= want) sh.found[1] = 1, sh.found[2] = key, sh.found[3] = eq, sh.found_mass[0] = over;
+                }
+                __syncthreads();
+                before = sh.found_mass[0], at = sh.found[2], same = sh.found[3];
+                return sh.found[1] != 0;
+            }
             uint32_t base = lo >> kGrain, size = (hi >> kGrain) - base + 1;  // the answer's cell lies in [base, base + size)
             before = above;
             for (bool first = true; first || size > 1; first = false) {
@@ -543,7 +590,8 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
                     Mass m;
                     part.each([&](int, const float *v) {
 #pragma unroll
-                        for (int e = 0; e < Part<T>::N; ++e) m.add_if(key_of(v[e]) > bound, w.of(v[e]));
+                        for (int e = 0; e < Part<T>::N; ++e)
+                            if (key_of(v[e]) > bound) m.add(Cut(w.of(v[e])));
                     });
                     total_of(m.units(), 0, 0, over, nullptr);
                     have = over.mass + (bound ? ties * w.units(value_of(bound)) : 0);
@@ -568,44 +616,52 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
         }
     }
 
+    const float cut_at = bound ? value_of(bound) : -INFINITY;
     auto kept = [&](float v, int pos, int last) -> float {
-        const uint32_t key = key_of(v);
-        if (key < bound || (key == bound && pos > last)) return 0.f;
+        if (!(v >= cut_at) || (bound && v == cut_at && pos > last)) return 0.f;
         if (greedy) return 1.f;
         const float x = w.of(v);
         return x < least ? 0.f : x;
     };
     const float u = a.uniform[row];
-    // The draw within a warp's stretch, `ahead` being the kept weight before it.
-    auto draw = [&](u64 ahead, u64 target, u64 total, int last) {
-        part.each([&](int pos, const float *v) {
-            u64 x[Part<T>::N], mine_sum = 0;
+    // The draw within the stretch of warp `owner`, `ahead` being the kept weight
+    // before it: every warp of the block takes one of its steps at a time.
+    auto draw = [&](int owner, u64 ahead, u64 target, u64 total, int last) {
+        constexpr int step = 32 * Part<T>::N;
+        for (int first = 0; first < warp_len; first += kWarps * step) {
+            const int p = owner * warp_len + first + warp * step + lane * Part<T>::N;
+            const bool in = first + warp * step < warp_len;
+            float v[Part<T>::N];
+            u64 x[Part<T>::N], sum = 0;
+            if (in) part.at(p, v);
 #pragma unroll
-            for (int e = 0; e < Part<T>::N; ++e) {
-                Mass one;
-                one.add(kept(v[e], pos + e, last));
-                x[e] = one.units(), mine_sum += x[e];
-            }
-            u64 incl = mine_sum;
+            for (int e = 0; e < Part<T>::N; ++e) x[e] = in ? Cut(kept(v[e], p + e, last)).units() : 0, sum += x[e];
+            u64 incl = sum;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const u64 up = shfl_up64(incl, o);
                 if (lane >= o) incl += up;
             }
-            u64 sum = ahead + incl - mine_sum;
+            __syncthreads();
+            if (lane == 31) sh.scan_mass[warp] = incl;
+            __syncthreads();
+            u64 at = ahead + incl - sum;
+            for (int q = 0; q < kWarps; ++q) {
+                if (q < warp) at += sh.scan_mass[q];
+                ahead += sh.scan_mass[q];
+            }
 #pragma unroll
             for (int e = 0; e < Part<T>::N; ++e) {
-                if (x[e] && sum <= target && sum + x[e] > target) {
-                    a.token[row] = part.begin + pos + e - part.skip;
+                if (x[e] && at <= target && at + x[e] > target) {
+                    a.token[row] = part.begin + p + e - part.skip;
                     if (a.logprob) {
                         const float share = (float)((double)total * (1.0 / (double)kUnit));
-                        a.logprob[row] = greedy ? 0.f : (w.top == INFINITY ? 0.f : (v[e] - w.top) / t) - logf(share);
+                        a.logprob[row] = greedy ? 0.f : (v[e] - w.top) / t - logf(share);
                     }
                 }
-                sum += x[e];
+                at += x[e];
             }
-            ahead += __shfl_sync(~0u, incl, 31);
-        });
+        }
     };
     auto target_of = [&](u64 total) {
         const u64 at = share_of(total, u, false);
@@ -619,8 +675,9 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
         const u64 unit = w.units(value_of(bound));
         if (warp < blocks) {
             uint32_t from = 0;
-            for (int r = 0; r < warp; ++r) from += *peer(&sh.listed[l], r);
-            const uint32_t n = *peer(&sh.listed[l], warp);
+            const uint32_t each = lane < blocks ? *peer(&sh.listed[l], lane % blocks) : 0;
+            from = __reduce_add_sync(~0u, lane < warp ? each : 0);
+            const uint32_t n = __shfl_sync(~0u, each, warp);
             u64 m = 0;
             uint32_t c = 0;
             for (uint32_t i = lane; i < n; i += 32) {
@@ -672,9 +729,13 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
             }
             __syncthreads();
             auto of_warp = [&](int q) { return sh.warp_base[q] + ((u64)sh.warp_hi[q] << 18) + sh.warp_lo[q]; };
-            for (int q = 0; q < warp; ++q) ahead += of_warp(q);
-            const u64 own = of_warp(warp);
-            if (target >= ahead && target - ahead < own) draw(ahead, target, total, (int)sh.found[0] - 1);
+            int owner = 0;
+            for (; owner + 1 < kWarps; ++owner) {
+                const u64 own = of_warp(owner);
+                if (target - ahead < own) break;
+                ahead += own;
+            }
+            draw(owner, ahead, target, total, (int)sh.found[0] - 1);
         }
         barrier();  // no block leaves while another may read its shared memory
         return;
@@ -724,15 +785,20 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
     Mass m;
     part.each([&](int pos, const float *v) {
 #pragma unroll
-        for (int e = 0; e < Part<T>::N; ++e) m.add(kept(v[e], pos + e, last_tie));
+        for (int e = 0; e < Part<T>::N; ++e) m.add(Cut(kept(v[e], pos + e, last_tie)));
     });
-    const u64 of_warp = warp_total(m.units());
     Sums all, before;
     total_of(m.units(), 0, 0, all, &before);
     const u64 target = target_of(all.mass);
     u64 ahead = before.mass;
-    for (int q = 0; q < warp; ++q) ahead += sh.warp_mass[q];
-    if (ahead <= target && ahead + of_warp > target) draw(ahead, target, all.mass, last_tie);  // one warp of the cluster
+    int owner = 0;
+    bool here = target >= ahead;
+    for (; here && owner < kWarps; ++owner) {
+        const u64 own = sh.warp_mass[owner];
+        if (target - ahead < own) break;
+        ahead += own;
+    }
+    if (here && owner < kWarps) draw(owner, ahead, target, all.mass, last_tie);  // one block of the cluster
     barrier();  // no block leaves while another may read its shared memory
 }
 
@@ -761,7 +827,9 @@ template <typename T> int run(const sim_op_sample_t *a, cudaStream_t st) {
     cfg.attrs = at, cfg.numAttrs = 1;
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = blocks, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_sample<T>, *a, warp_len, staged);
+    int bins = kThreads;  // about 32 logits each
+    while (bins < kCoarse && bins * 32 < a->vocab) bins *= 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_sample<T>, *a, warp_len, staged, bins);
     return e == cudaSuccess ? SIM_OK : fail(SIM_ERR_CUDA, "sim_op_sample: %s", cudaGetErrorString(e));
 }
 
