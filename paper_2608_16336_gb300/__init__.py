@@ -28,4 +28,4 @@ Draining (Sec. 3.5) is an input: set ``w.drain_start_us`` to a uint32
 [replicas, instances] array of start times (0xFFFFFFFF = never) before
 ``load``.  ``workloads.custom`` builds a workload from explicit traces.
 """
-__all__ = ["workloads", "mtsim", "instance_ops", "instance"]
+__all__ = ["workloads", "mtsim"]

@@ -43,6 +43,7 @@ EXPORTS = ["sim_op_rotary", "sim_op_latent_append", "sim_op_latent_decode", "sim
            "sim_op_latent_prefill", "sim_op_sample", "sim_op_faults", "sim_op_last_error"]
 
 _LIB = None
+_WORKSPACE: dict[tuple, int] = {}  # bytes by sizes
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
@@ -64,27 +65,29 @@ def lib() -> ctypes.CDLL:
     return _LIB
 
 
-def _check(code: int) -> None:
-    if code != mtsim.SIM_OK:
-        raise mtsim.SimError(code, lib().sim_op_last_error().decode())
+def _failed(code: int):
+    raise mtsim.SimError(code, lib().sim_op_last_error().decode())
 
 
 def faults() -> int:
     """Waits inside the operators' kernels that ran out (0 unless a kernel is at fault); synchronises the device."""
     n = lib().sim_op_faults()
     if n < 0:
-        _check(n)
+        _failed(n)
     return n
 
 
-def _place(*tensors) -> int:
-    """The one CUDA device, the current one, that every tensor is on."""
+def _place(tensors, others=()) -> int:
+    """The one CUDA device, the current one, that every tensor is on; ``tensors`` may not ask for gradients."""
     device = tensors[0].get_device()
     for t in tensors:
         if t.get_device() != device:
             raise ValueError("every tensor must be on the same CUDA device")
         if t.requires_grad and torch.is_grad_enabled():
             raise ValueError("forward only: call under torch.no_grad() or detach the tensors")
+    for t in others:
+        if t.get_device() != device:
+            raise ValueError("every tensor must be on the same CUDA device")
     if device < 0:
         raise ValueError("the tensors must be on a CUDA device")
     if device != _current_device():
@@ -103,27 +106,27 @@ def _type(name, t, *others, wide=True) -> int:
 
 
 def _packed(name, t, shape) -> None:
-    if t.shape != shape:
-        raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
-    if not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be contiguous with shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
 
 
 def _rows(name, t, shape):
     """The strides of a tensor of that shape whose last dimension is contiguous."""
+    s = t.stride()
     if t.shape != shape:
         raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
-    s = t.stride()
-    if s[-1] != 1 and t.shape[-1] > 1:
+    if s[-1] != 1 and shape[-1] > 1:
         raise ValueError("the last dimension of %s must be contiguous" % name)
     return s
 
 
 def _positions(t, n) -> int:
-    if t.dtype is not torch.int32 and t.dtype is not torch.int64:
-        raise TypeError("positions must be int32 or int64, not %s" % t.dtype)
-    _packed("positions", t, (n,))
-    return int(t.dtype is torch.int64)
+    kind = t.dtype
+    if kind is not torch.int32 and kind is not torch.int64:
+        raise TypeError("positions must be int32 or int64, not %s" % kind)
+    if t.shape != (n,) or not t.is_contiguous():
+        raise ValueError("positions must be a contiguous vector of %d values" % n)
+    return 1 if kind is torch.int64 else 0
 
 
 def _frequencies(t) -> int:
@@ -182,21 +185,24 @@ def rotary(x, positions, frequencies, *, layout="interleaved", offset=0, amplitu
     every head of ``x`` [tokens, heads, dim].  ``out=x`` works in place; the
     default is a new tensor, the other elements copied."""
     rot = _frequencies(frequencies)
-    if x.dim() != 3:
+    shape = x.shape
+    if len(shape) != 3:
         raise ValueError("x must be [tokens, heads, dim]")
-    n, heads, dim = x.shape
+    n, heads, dim = shape
     if offset < 0 or offset + rot > dim:
         raise ValueError("elements [%d, %d) do not lie in a head of %d" % (offset, offset + rot, dim))
     wide = _positions(positions, n)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    xs, ys = _rows("x", x, x.shape), _rows("out", out, x.shape)
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+    xs, ys = _rows("x", x, shape), _rows("out", out, shape)
     code = _type("x", x, out)
-    device = _place(x, out, positions, frequencies)
-    _check(lib().sim_op_rotary(
+    device = _place((x, out), (positions, frequencies))
+    rc = (_LIB or lib()).sim_op_rotary(
         ROTARY.pack(x.data_ptr(), out.data_ptr(), positions.data_ptr(), frequencies.data_ptr(), n, xs[0], xs[1], ys[0], ys[1],
                     heads, dim, rot, offset, code, _layout(layout), wide, 1 if inverse else 0, amplitude),
-        _stream_of(device)))
+        _stream_of(device))
+    if rc:
+        _failed(rc)
     return out
 
 
@@ -216,12 +222,14 @@ def latent_append(latent, key, positions, frequencies, slots, cache, *, layout="
         raise TypeError("slots must be int64, not %s" % slots.dtype)
     _packed("slots", slots, (n,))
     code = _type("latent", latent, key, cache)
-    device = _place(latent, key, positions, frequencies, slots, cache)
-    _check(lib().sim_op_latent_append(
+    device = _place((latent, key, cache), (positions, frequencies, slots))
+    rc = (_LIB or lib()).sim_op_latent_append(
         APPEND.pack(latent.data_ptr(), key.data_ptr(), cache.data_ptr(), positions.data_ptr(), slots.data_ptr(),
                     frequencies.data_ptr(), n, ls[0], ks[0], cs[0], cs[1], blocks, block, rank, rot, code, _layout(layout), wide,
                     amplitude),
-        _stream_of(device)))
+        _stream_of(device))
+    if rc:
+        _failed(rc)
     return cache
 
 
@@ -256,15 +264,20 @@ def latent_decode(q, cache, table, lengths, *, scale, out=None, lse=None):
         raise TypeError("lse must be float32")
     _packed("lse", lse, (b, new, heads))
     code = _type("q", q, cache, out, wide=False)
-    device = _place(q, cache, table, lengths, out, lse)
-    L = lib()
-    nbytes = L.sim_op_latent_decode_workspace(b, new, heads, rank)
-    work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-    _check(L.sim_op_latent_decode(
+    device = _place((q, cache, out, lse), (table, lengths))
+    L = _LIB or lib()
+    size = (device, b, new, heads, rank)
+    nbytes = _WORKSPACE.get(size)
+    if nbytes is None:
+        nbytes = _WORKSPACE[size] = L.sim_op_latent_decode_workspace(b, new, heads, rank)
+    work = lse.new_empty(nbytes // 4 + 1)
+    rc = L.sim_op_latent_decode(
         DECODE.pack(q.data_ptr(), cache.data_ptr(), table.data_ptr(), lengths.data_ptr(), out.data_ptr(), lse.data_ptr(),
                     work.data_ptr(), nbytes, qs[0], qs[1], qs[2], os_[0], os_[1], os_[2], cs[0], cs[1], ts[0], blocks, b, new,
                     heads, rank, width - rank, block, table.shape[1], code, scale),
-        _stream_of(device)))
+        _stream_of(device))
+    if rc:
+        _failed(rc)
     return out, lse
 
 
@@ -302,12 +315,14 @@ def latent_prefill(q, key, shared, value, q_offsets, k_offsets, *, scale, longes
         raise TypeError("lse must be float32")
     _packed("lse", lse, (n, heads))
     code = _type("q", q, key, shared, value, out, wide=False)
-    device = _place(q, key, shared, value, q_offsets, k_offsets, out, lse)
-    _check(lib().sim_op_latent_prefill(
+    device = _place((q, key, shared, value, out, lse), (q_offsets, k_offsets))
+    rc = (_LIB or lib()).sim_op_latent_prefill(
         PREFILL.pack(q.data_ptr(), key.data_ptr(), shared.data_ptr(), value.data_ptr(), q_offsets.data_ptr(),
                      k_offsets.data_ptr(), out.data_ptr(), lse.data_ptr(), qs[0], qs[1], ks[0], ks[1], ss[0], vs[0], vs[1],
                      os_[0], os_[1], n, m, b, heads, longest, head, rot, wide, 1 if causal else 0, code, scale),
-        _stream_of(device)))
+        _stream_of(device))
+    if rc:
+        _failed(rc)
     return out, lse
 
 
@@ -347,6 +362,8 @@ def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=N
     args = SAMPLE.pack(logits.data_ptr(), vector("uniform", uniform, real), vector("temperature", temperature, real),
                        vector("top_k", top_k, torch.int32), vector("top_p", top_p, real), vector("min_p", min_p, real),
                        vector("out", out, torch.int64), vector("logprob", logprob, real), stride, rows, vocab, code)
-    _place(logits)
-    _check(lib().sim_op_sample(args, _stream_of(device)))
+    _place((logits,))
+    rc = (_LIB or lib()).sim_op_sample(args, _stream_of(device))
+    if rc:
+        _failed(rc)
     return out, logprob
