@@ -26,6 +26,7 @@ constexpr int kBinsEach = kCoarse / kThreads;
 constexpr float kUnit = 1099511627776.f, kUnitLog2 = 40.f;
 constexpr int kMostCluster = 8;
 constexpr int kMostStaged = 180 * 1024;  // bytes of a block's part
+constexpr int kHalfStaged = 72 * 1024;   // of one that leaves room for another block
 
 // Order-preserving whole number of a logit (not NaN); -0 ranks with 0.
 __device__ __forceinline__ uint32_t key_of(float v) {
@@ -271,21 +272,31 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
             }
         });
         barrier();
-        // a thread has some neighbouring bins; counts and approximate weight up to
-        // and with them.  (Every block begins with its own: all reading the same one's memory at a time takes twice as long.)
+        // Sums of the blocks' bins: each block adds up its share of the bins (in
+        // place: no other reads those of it) and then all take every share.
+        const int share = bins / blocks;
+        if (blocks > 1) {
+            for (int b = rank * share + threadIdx.x; b < (rank + 1) * share; b += kThreads) {
+                uint32_t c = 0;
+#pragma unroll 4
+                for (int q = 0; q < blocks; ++q) c += *peer(&sh.coarse[b], (rank + q) % blocks);
+                sh.coarse[b] = c;
+            }
+            barrier();
+        }
+        // a thread has some neighbouring bins; counts and approximate weight up to and with them
         const int each_bins = bins / kThreads, first_bin = each_bins * threadIdx.x;
         uint32_t bin_count[kBinsEach] = {};
-        for (int q = 0; q < blocks; ++q) {
-            const int r = rank + q < blocks ? rank + q : rank + q - blocks;
-            const uint32_t *from = peer(&sh.coarse[first_bin], r);
+        {
+            const uint32_t *from = peer(&sh.coarse[first_bin], first_bin / share);
             if (each_bins == 8) {
                 const uint4 c = *(const uint4 *)from, d = *(const uint4 *)(from + 4);
-                bin_count[0] += c.x, bin_count[1] += c.y, bin_count[2] += c.z, bin_count[3] += c.w;
-                bin_count[4] += d.x, bin_count[5] += d.y, bin_count[6] += d.z, bin_count[7] += d.w;
+                bin_count[0] = c.x, bin_count[1] = c.y, bin_count[2] = c.z, bin_count[3] = c.w;
+                bin_count[4] = d.x, bin_count[5] = d.y, bin_count[6] = d.z, bin_count[7] = d.w;
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (e < each_bins) bin_count[e] += from[e];
+                    if (e < each_bins) bin_count[e] = from[e];
             }
         }
         auto bin_weight = [&](int bin) { return exp2_near(40.f - bin / fine); };  // bins are about their middles
@@ -805,14 +816,15 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
 template <typename T> int run(const sim_op_sample_t *a, cudaStream_t st) {
     const int sms = sm_count();
     if (!sms) return SIM_ERR_CUDA;
-    // As many blocks a row as still run all at once (two a multiprocessor),
-    // while a block's part is 2,048 logits or more.
+    // Blocks a row: so many that two blocks' parts fit in a multiprocessor's shared
+    // memory (128 x 131,075 bfloat16: 4 blocks 86 us, 2 blocks 101), and more while all
+    // rows' blocks still run at once and a part is 2,048 logits or more (64 rows of
+    // that: 4 blocks 45 us, 8 blocks 65; 1 x 32,000: 8 blocks 21 us, 2 blocks 25).
     constexpr int N = 16 / sizeof(T);
     int blocks = 1;
-    while (blocks < kMostCluster && (int64_t)a->rows * blocks * 2 <= 2 * sms && a->vocab / (blocks * 2) >= 2048) blocks *= 2;
-    // more where the part would not fit in shared memory
     auto stretch = [&](int n) { return (int)(((int64_t)a->vocab + N - 1 + (int64_t)n * kWarps * 32 * N - 1) / ((int64_t)n * kWarps * 32 * N)) * 32 * N; };
-    while (blocks < kMostCluster && (int64_t)stretch(blocks) * kWarps * (int)sizeof(T) > kMostStaged) blocks *= 2;
+    while (blocks < kMostCluster && (int64_t)stretch(blocks) * kWarps * (int)sizeof(T) > kHalfStaged) blocks *= 2;
+    while (blocks < kMostCluster && (int64_t)a->rows * blocks * 2 <= 2 * sms && a->vocab / (blocks * 2) >= 2048) blocks *= 2;
     const int warp_len = stretch(blocks);
     const int64_t bytes = (int64_t)warp_len * kWarps * sizeof(T);
     const bool staged = bytes <= kMostStaged;
