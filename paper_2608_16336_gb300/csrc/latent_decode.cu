@@ -121,8 +121,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
     const int rt = blockIdx.x % a.row_tiles, part = blockIdx.x / a.row_tiles;
     const int value_blocks = a.rank / 64, half = min(4, value_blocks);
     bool dead = false;
-    asm volatile("griddepcontrol.launch_dependents;");
+    let_next_start();
 
+    if (warp == 1 && lane == 0) {
+        for (int s = 0; s < a.stages; ++s) {
+            bar_init(smem_addr(&bars->full[s]), 1);
+            bar_init(smem_addr(&bars->empty[s][0]), a.pair ? 2 : 1);
+            bar_init(smem_addr(&bars->empty[s][1]), a.pair ? 2 : 1);
+        }
+        bar_init(smem_addr(&bars->q_full), a.q_flat ? 1 : 64);
+        bar_init(smem_addr(&bars->q_empty), 1);
+        for (int s = 0; s < Z::scores; ++s) bar_init(smem_addr(&bars->s_ready[s]), 1);
+        for (int s = 0; s < Z::weights; ++s) {
+            bar_init(smem_addr(&bars->p_ready[s]), kSoftWarps * 32);
+            bar_init(smem_addr(&bars->pv_done[s]), 1);
+        }
+        bar_init(smem_addr(&bars->o_free), kSoftWarps * 32);
+        bar_init_done();
+    }
+    if (warp == kSoftWarps) tmem_alloc(smem_addr(&bars->tmem), kCols);
+    if (warp == kSoftWarps + 1 && lane == 0) fetch_map(&m_cache), fetch_map(&m_q);
+    __syncwarp();
+    after_previous();
     if (warp == 0) {
         // the line's length, and where this part begins on it; a lane keeps the
         // tiles of its first requests, so that most calls read the lengths once
@@ -152,24 +172,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
         if (lane == 0) {
             bars->total = total;
             if (blockIdx.x == 0) a.first[a.requests] = total;
-            for (int s = 0; s < a.stages; ++s) {
-                bar_init(smem_addr(&bars->full[s]), 1);
-                bar_init(smem_addr(&bars->empty[s][0]), a.pair ? 2 : 1);
-                bar_init(smem_addr(&bars->empty[s][1]), a.pair ? 2 : 1);
-            }
-            bar_init(smem_addr(&bars->q_full), a.q_flat ? 1 : 64);
-            bar_init(smem_addr(&bars->q_empty), 1);
-            for (int s = 0; s < Z::scores; ++s) bar_init(smem_addr(&bars->s_ready[s]), 1);
-            for (int s = 0; s < Z::weights; ++s) {
-                bar_init(smem_addr(&bars->p_ready[s]), kSoftWarps * 32);
-                bar_init(smem_addr(&bars->pv_done[s]), 1);
-            }
-            bar_init(smem_addr(&bars->o_free), kSoftWarps * 32);
-            bar_init_done();
         }
     }
-    if (warp == kSoftWarps) tmem_alloc(smem_addr(&bars->tmem), kCols);
-    if (warp == kSoftWarps + 1 && lane == 0) fetch_map(&m_cache), fetch_map(&m_q);
     __syncwarp();
     tmem_before_sync();
     if (a.pair) cluster_sync();
@@ -531,7 +535,8 @@ constexpr int kJoinWarps = 8;
 
 template <typename T, int WARPS> __global__ void __launch_bounds__(kJoinWarps * 32) k_join(const __grid_constant__ Args a) {
     __shared__ float4 sum_of[WARPS > 1 ? kJoinWarps : 1][SIM_OP_MAX_RANK / 4];
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // the parts are written
+    let_next_start();
+    after_previous();  // the parts are written
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, mine = warp % WARPS;
     const int rows = a.new_tokens * a.heads;
     const int64_t row = (int64_t)blockIdx.x * (kJoinWarps / WARPS) + warp / WARPS;
@@ -623,30 +628,14 @@ template <typename T> int run(const Args &k, const CUtensorMap &m_cache, const C
     auto kernel = k.tile == 32 ? k_decode<T, 32> : k_decode<T, 64>;
     static std::atomic<uint64_t> told[2];
     if (!allow_shared((const void *)kernel, kShared, told[k.tile == 32])) return SIM_ERR_CUDA;
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
-    cfg.gridDim = dim3(c.row_tiles * c.lanes);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kShared;
-    cfg.stream = st;
-    cfg.attrs = at, cfg.numAttrs = k.pair ? 1 : 0;
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = 2, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, k, m_cache, m_q);
-    if (e != cudaSuccess) return fail(SIM_ERR_CUDA, "sim_op_latent_decode: %s", cudaGetErrorString(e));
+    cudaError_t e = launch_early(kernel, c.row_tiles * c.lanes, kThreads, kShared, k.pair ? 2 : 1, st, k, m_cache, m_q);
+    if (e != cudaSuccess) return launched("sim_op_latent_decode", e);
     // A row has about lanes / requests pieces: many are shared by a block's
-    // warps, few are one warp's.  The join's blocks start while the last parts run,
-    // and wait for them.
+    // warps, few are one warp's.
     const bool many = c.lanes > 8 * (int64_t)k.requests;
     const int64_t rows = (int64_t)k.requests * k.new_tokens * k.heads, per = many ? 1 : kJoinWarps;
-    cfg.gridDim = dim3((unsigned)((rows + per - 1) / per));
-    cfg.blockDim = dim3(kJoinWarps * 32);
-    cfg.dynamicSmemBytes = 0;
-    cfg.numAttrs = 1;
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    e = cudaLaunchKernelEx(&cfg, many ? k_join<T, kJoinWarps> : k_join<T, 1>, k);
-    return e == cudaSuccess ? SIM_OK : fail(SIM_ERR_CUDA, "sim_op_latent_decode (join): %s", cudaGetErrorString(e));
+    e = launch_early(many ? k_join<T, kJoinWarps> : k_join<T, 1>, (unsigned)((rows + per - 1) / per), kJoinWarps * 32, 0, 1, st, k);
+    return launched("sim_op_latent_decode (join)", e);
 }
 
 }  // namespace

@@ -72,6 +72,8 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     const uint32_t q_at = smem_addr(smem), ring = q_at + ring_offset;
     Barriers *bars = (Barriers *)(smem + ring_offset + kSlots * kSlotBytes);
 
+    let_next_start();
+    after_previous();
     // which rows: within a group of heads the last (longest) row blocks come first
     int item = blockIdx.x;
     const int per_request = a.row_blocks * a.heads;
@@ -369,8 +371,8 @@ template <typename T, int TILES>
 int run(const Args &k, const CUtensorMap *m, unsigned grid, cudaStream_t st) {
     static std::atomic<uint64_t> told;
     if (!allow_shared((const void *)k_prefill<T, TILES>, Shape<TILES>::shared, told)) return SIM_ERR_CUDA;
-    k_prefill<T, TILES><<<grid, Shape<TILES>::threads, Shape<TILES>::shared, st>>>(k, m[0], m[1], m[2], m[3], m[4]);
-    return launched("sim_op_latent_prefill");
+    const cudaError_t e = launch_early(k_prefill<T, TILES>, grid, Shape<TILES>::threads, Shape<TILES>::shared, 1, st, k, m[0], m[1], m[2], m[3], m[4]);
+    return launched("sim_op_latent_prefill", e);
 }
 
 }  // namespace

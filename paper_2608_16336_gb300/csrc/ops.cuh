@@ -17,13 +17,31 @@ namespace mtop {
 int fail(int code, const char *fmt, ...);
 
 // The launch's error, or SIM_OK.
-inline int launched(const char *what) {
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? SIM_OK : fail(SIM_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+inline int launched(const char *what, cudaError_t e) {
+    if (e == cudaSuccess) return SIM_OK;
+    cudaGetLastError();  // the caller has it from here: it is not left for the next one that asks
+    return fail(SIM_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
 // Lets a kernel use that much shared memory; `done` (one a kernel) keeps which devices have been told.
 bool allow_shared(const void *kernel, int bytes, std::atomic<uint64_t> &done);
+
+// Launches a kernel whose blocks may be set up while the one ahead of it in
+// the stream still runs.  Every thread calls after_previous() before it reads
+// or writes anything that is not its own, so that the stream's order holds;
+// two calls in a row save 2 us of 15 to 100.
+template <typename... P, typename... A>
+inline cudaError_t launch_early(void (*kernel)(P...), unsigned grid, int threads, size_t shared, int cluster, cudaStream_t st, const A &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[2];
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(threads), cfg.dynamicSmemBytes = shared, cfg.stream = st;
+    cfg.attrs = at, cfg.numAttrs = cluster > 1 ? 2 : 1;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 // SMs of the current device (152 on a whole GB300), or 0 with an error set.
 int sm_count();
@@ -94,6 +112,11 @@ __device__ __forceinline__ void angle_cos_sin(unsigned long long turns, long lon
 
 // Barrier `id` of the block's first (or other) `threads` threads.
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// The kernels before this one in the stream have ended and what they wrote is
+// visible; the one after it may start (and wait here) from now on.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;"); }
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll

@@ -14,6 +14,8 @@ __global__ void __launch_bounds__(256) k_rotary(sim_op_rotary_t a) {
     const T *x = (const T *)a.x;
     T *out = (T *)a.out;
     const int half = a.rot_dim / 2;
+    let_next_start();
+    after_previous();
     for (int64_t n = blockIdx.x; n < a.tokens; n += gridDim.x) {
         const int64_t p = a.positions_64 ? ((const int64_t *)a.positions)[n] : ((const int32_t *)a.positions)[n];
         __syncthreads();
@@ -83,6 +85,8 @@ __global__ void __launch_bounds__(kRotaryWarps * 32) k_rotary_wide(const __grid_
     constexpr int N = Vec<T>::N, P = HALF ? N : N / 2;  // pairs of a thread
     __shared__ float2 turn[SIM_OP_MAX_ROT / 2];
     const int half = a.rot_dim / 2, turned = a.rot_dim / N / (HALF ? 2 : 1), rest = (a.dim - a.rot_dim) / N;
+    let_next_start();
+    after_previous();
     const bool turns = (int)threadIdx.x < turn_warps * 32;
     const int units = turns ? turned : rest, threads = turns ? turn_warps * 32 : (kRotaryWarps - turn_warps) * 32;
     const int id = turns ? threadIdx.x : threadIdx.x - turn_warps * 32;
@@ -143,6 +147,8 @@ __global__ void __launch_bounds__(kRotaryWarps * 32) k_rotary_wide(const __grid_
 template <typename T>
 __global__ void __launch_bounds__(128) k_append(sim_op_latent_append_t a) {
     const int half = a.rot_dim / 2;
+    let_next_start();
+    after_previous();
     for (int64_t n = blockIdx.x; n < a.tokens; n += gridDim.x) {
         const int64_t slot = a.slots[n];
         if (slot < 0 || slot >= a.blocks * a.block_tokens) continue;
@@ -176,6 +182,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32, 6) k_append_wide(const __gr
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int half = a.rot_dim / 2, turned = a.rot_dim / N / (HALF ? 2 : 1), copied = a.rank / N;
     float2 *turn = turns[warp];
+    let_next_start();
+    after_previous();
     const unsigned long long per = lane < half ? turns_per_position(a.frequencies[lane]) : 0;
     const int64_t rows = a.blocks * a.block_tokens;
     for (int64_t n = (int64_t)blockIdx.x * kAppendWarps + warp; n < a.tokens; n += (int64_t)gridDim.x * kAppendWarps) {
@@ -234,30 +242,30 @@ template <typename T> int run_rotary(const sim_op_rotary_t *a, cudaStream_t st) 
     // warps in proportion to the bytes they move; in place nothing is copied
     int turn_warps = a->x == a->out || rest == 0 ? kRotaryWarps : (kRotaryWarps * a->rot_dim + a->dim / 2) / a->dim;
     turn_warps = turn_warps < 1 ? 1 : turn_warps > kRotaryWarps - (rest && a->x != a->out) ? kRotaryWarps - (rest && a->x != a->out) : turn_warps;
+    cudaError_t e;
     if (whole(N, {a->x, a->out}, {a->x_token, a->x_head, a->out_token, a->out_head, a->dim, a->rot_offset, half ? a->rot_dim / 2 : a->rot_dim}) &&
         turned <= 32 * turn_warps && (turn_warps == kRotaryWarps || rest <= 32 * (kRotaryWarps - turn_warps))) {
-        const int grid = (int)(a->tokens < 16384 ? a->tokens : 16384);
-        if (half) k_rotary_wide<T, true><<<grid, kRotaryWarps * 32, 0, st>>>(*a, turn_warps);
-        else k_rotary_wide<T, false><<<grid, kRotaryWarps * 32, 0, st>>>(*a, turn_warps);
+        const unsigned grid = (unsigned)(a->tokens < 16384 ? a->tokens : 16384);
+        e = launch_early(half ? k_rotary_wide<T, true> : k_rotary_wide<T, false>, grid, kRotaryWarps * 32, 0, 1, st, *a, turn_warps);
     } else {
-        k_rotary<T><<<(int)(a->tokens < (1 << 20) ? a->tokens : (1 << 20)), 256, 0, st>>>(*a);
+        e = launch_early(k_rotary<T>, (unsigned)(a->tokens < (1 << 20) ? a->tokens : (1 << 20)), 256, 0, 1, st, *a);
     }
-    return launched("sim_op_rotary");
+    return launched("sim_op_rotary", e);
 }
 
 template <typename T> int run_append(const sim_op_latent_append_t *a, int sms, cudaStream_t st) {
     constexpr int N = 16 / sizeof(T);
     const bool half = a->layout == SIM_OP_HALF;
+    cudaError_t e;
     if (whole(N, {a->latent, a->key, a->cache},
               {a->latent_token, a->key_token, a->cache_block, a->cache_row, a->rank, half ? a->rot_dim / 2 : a->rot_dim})) {
         const int64_t want = (a->tokens + kAppendWarps - 1) / kAppendWarps, most = 6 * (int64_t)sms;
-        const int grid = (int)(want < most ? want : most);
-        if (half) k_append_wide<T, true><<<grid, kAppendWarps * 32, 0, st>>>(*a);
-        else k_append_wide<T, false><<<grid, kAppendWarps * 32, 0, st>>>(*a);
+        const unsigned grid = (unsigned)(want < most ? want : most);
+        e = launch_early(half ? k_append_wide<T, true> : k_append_wide<T, false>, grid, kAppendWarps * 32, 0, 1, st, *a);
     } else {
-        k_append<T><<<(int)(a->tokens < (1 << 20) ? a->tokens : (1 << 20)), 128, 0, st>>>(*a);
+        e = launch_early(k_append<T>, (unsigned)(a->tokens < (1 << 20) ? a->tokens : (1 << 20)), 128, 0, 1, st, *a);
     }
-    return launched("sim_op_latent_append");
+    return launched("sim_op_latent_append", e);
 }
 
 bool bad_type(int t) { return t != SIM_OP_BF16 && t != SIM_OP_FP16 && t != SIM_OP_FP32; }

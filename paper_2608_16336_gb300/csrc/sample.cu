@@ -180,6 +180,8 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
     part.held = nullptr, part.endless = false;
     T *const mine = (T *)dynamic;
 
+    let_next_start();
+    after_previous();
     int turn = 0;  // which of the two exchange buffers
     auto barrier = [&]() {
         if (blocks > 1) cluster.sync();
@@ -830,19 +832,10 @@ template <typename T> int run(const sim_op_sample_t *a, cudaStream_t st) {
     const bool staged = bytes <= kMostStaged;
     static std::atomic<uint64_t> told;
     if (!allow_shared((const void *)k_sample<T>, kMostStaged, told)) return SIM_ERR_CUDA;
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
-    cfg.gridDim = dim3((unsigned)a->rows * blocks);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = staged ? (size_t)bytes : 0;
-    cfg.stream = st;
-    cfg.attrs = at, cfg.numAttrs = 1;
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = blocks, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
     int bins = kThreads;  // about 32 logits each
     while (bins < kCoarse && bins * 32 < a->vocab) bins *= 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_sample<T>, *a, warp_len, staged, bins);
-    return e == cudaSuccess ? SIM_OK : fail(SIM_ERR_CUDA, "sim_op_sample: %s", cudaGetErrorString(e));
+    const cudaError_t e = launch_early(k_sample<T>, (unsigned)a->rows * blocks, kThreads, staged ? (size_t)bytes : 0, blocks, st, *a, warp_len, staged, bins);
+    return launched("sim_op_sample", e);
 }
 
 }  // namespace
