@@ -458,7 +458,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
             const bool whole = pc.t0 == 0 && pc.t1 == pc.n;
             // an unfinished piece: the part's last if it begins the request, else its first
             const int64_t slot = (int64_t)blockIdx.x * 2 + (pc.t0 == 0);
-            const float inv0 = sum0 > 0.f ? 1.f / sum0 : 0.f, inv1 = sum1 > 0.f ? 1.f / sum1 : 0.f;
+            // (a sum of 0 is a row that sees nothing: zeros; one that is no number stays so)
+            const float inv0 = sum0 != 0.f ? 1.f / sum0 : 0.f, inv1 = sum1 != 0.f ? 1.f / sum1 : 0.f;
             float *sums = a.sums + (slot * kRows + warp * 16) * a.rank;
             T *out = (T *)a.out + pc.b * a.out_request;
             // Fragments hold 8 bytes of a row; through the (now idle) rows of P
@@ -472,8 +473,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const uint32_t chunk = (uint32_t)((e ^ swz) << 4);
-                        const uint32_t w0 = sum0 > 0.f ? pack2<T>(v[4 * e] * inv0, v[4 * e + 1] * inv0) : 0u;
-                        const uint32_t w1 = sum1 > 0.f ? pack2<T>(v[4 * e + 2] * inv1, v[4 * e + 3] * inv1) : 0u;
+                        const uint32_t w0 = sum0 != 0.f ? pack2<T>(v[4 * e] * inv0, v[4 * e + 1] * inv0) : 0u;
+                        const uint32_t w1 = sum1 != 0.f ? pack2<T>(v[4 * e + 2] * inv1, v[4 * e + 3] * inv1) : 0u;
                         asm volatile("st.shared.b32 [%0], %1;" ::"r"(p0 + chunk), "r"(w0) : "memory");
                         asm volatile("st.shared.b32 [%0], %1;" ::"r"(p1 + chunk), "r"(w1) : "memory");
                     }
@@ -512,8 +513,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
             if (lane % 4 == 0) {
                 if (whole) {
                     const int64_t at = (int64_t)pc.b * a.new_tokens * a.heads;
-                    if (real0 && a.lse) a.lse[at + f0] = sum0 > 0.f ? (top0 + log2f(sum0)) * 0.6931471805599453f : -INFINITY;
-                    if (real1 && a.lse) a.lse[at + f1] = sum1 > 0.f ? (top1 + log2f(sum1)) * 0.6931471805599453f : -INFINITY;
+                    if (real0 && a.lse) a.lse[at + f0] = sum0 != 0.f ? (top0 + log2f(sum0)) * 0.6931471805599453f : -INFINITY;
+                    if (real1 && a.lse) a.lse[at + f1] = sum1 != 0.f ? (top1 + log2f(sum1)) * 0.6931471805599453f : -INFINITY;
                 } else {
                     a.stats[slot * kRows + r0] = make_float2(top0, sum0);
                     a.stats[slot * kRows + r0 + 8] = make_float2(top1, sum1);
@@ -594,15 +595,15 @@ template <typename T, int WARPS> __global__ void __launch_bounds__(kJoinWarps * 
                 v[j].x += u.x, v[j].y += u.y, v[j].z += u.z, v[j].w += u.w;
             }
     }
-    const float inv = all > 0.f ? 1.f / all : 0.f;
+    const float inv = all != 0.f ? 1.f / all : 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (128 * j + 4 * lane < a.rank) {
             uint2 w = make_uint2(0, 0);
-            if (all > 0.f) w = make_uint2(pack2<T>(v[j].x * inv, v[j].y * inv), pack2<T>(v[j].z * inv, v[j].w * inv));
+            if (all != 0.f) w = make_uint2(pack2<T>(v[j].x * inv, v[j].y * inv), pack2<T>(v[j].z * inv, v[j].w * inv));
             *(uint2 *)(out + 128 * j + 4 * lane) = w;
         }
-    if (a.lse && lane == 0) a.lse[row] = all > 0.f ? (m + log2f(all)) * 0.6931471805599453f : -INFINITY;
+    if (a.lse && lane == 0) a.lse[row] = all != 0.f ? (m + log2f(all)) * 0.6931471805599453f : -INFINITY;
 }
 
 // How the work is cut: row tiles side by side, and parts of the line of tiles.

@@ -331,9 +331,10 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             bar_arrive(smem_addr(&bars->p_ready[t]));
             sum += (s0 + s1) + (s2 + s3);
         }
+        // a sum of 0 is a row that sees nothing: zeros; a sum that is no number stays one
         if (row < rows && a.lse)
-            a.lse[(int64_t)(q0 + row) * a.heads + h] = sum > 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+            a.lse[(int64_t)(q0 + row) * a.heads + h] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        const float inv = sum != 0.f ? 1.f / sum : 0.f;
         T *out = (T *)a.out + (int64_t)(q0 + row) * a.out_row + h * a.out_head;
         if (nt > 0) {
             bar_wait(smem_addr(&bars->o_ready[t]), 0, dead);
@@ -352,7 +353,7 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
                     for (int e = 0; e < 32; e += 8)
                         if (32 * c + e < a.value_dim) {
                             uint4 w;
-                            auto val = [&](int j) { return sum > 0.f ? __uint_as_float(o[e + j]) * inv : 0.f; };
+                            auto val = [&](int j) { return sum != 0.f ? __uint_as_float(o[e + j]) * inv : 0.f; };
                             w.x = pack2<T>(val(0), val(1)), w.y = pack2<T>(val(2), val(3));
                             w.z = pack2<T>(val(4), val(5)), w.w = pack2<T>(val(6), val(7));
                             *(uint4 *)(out + 32 * c + e) = w;

@@ -270,6 +270,19 @@ def test_decode_table_and_lengths_out_of_range():
     assert not out[0].any() and (lse[0] == -math.inf).all()
 
 
+@pytest.mark.parametrize("lengths", [[60, 40], [5000, 40]])  # whole requests, and joined parts
+@pytest.mark.parametrize("junk", [float("nan"), float("inf")])
+def test_decode_numbers_that_are_none_show(lengths, junk):
+    """A score that is NaN or +infinity makes the row's result NaN, not zero; other requests keep theirs."""
+    q, cache, table, n = decode_case(lengths, 1, 16, 512, 64, 16, BF, seed=13)
+    want, lse = ops.latent_decode(q, cache, table, n, scale=0.05)
+    q[0, 0, 3, 100] = 1.0
+    cache[int(table[0, 1]), 5, 100] = junk
+    out, lse2 = ops.latent_decode(q, cache, table, n, scale=0.05)
+    assert out[0, 0, 3].isnan().all() and lse2[0, 0, 3].isnan()
+    assert torch.equal(out[1], want[1]) and torch.equal(lse2[1], lse[1])
+
+
 def test_decode_strides():
     g = gen(6)
     q, cache, table, n = decode_case([150, 40], 2, 6, 512, 64, 16, BF, seed=6)
@@ -413,6 +426,18 @@ def test_prefill_later_keys_do_not_count():
     args[1][150:] = float("nan")
     out, lse2 = ops.latent_prefill(*args, scale=0.1, longest=200)
     assert torch.equal(out[:150], want[:150]) and torch.equal(lse2[:150], lse[:150])
+
+
+@pytest.mark.parametrize("nk", [200, 3000])
+@pytest.mark.parametrize("junk", [float("nan"), float("inf")])
+def test_prefill_numbers_that_are_none_show(nk, junk):
+    args = prefill_case([200], [nk], 2, 128, 64, 128, BF, seed=2)
+    want, lse = ops.latent_prefill(*args, scale=0.1, longest=200)
+    args[0][:, 1, 7] = 1.0
+    args[1][nk - 50, 1, 7] = junk
+    out, lse2 = ops.latent_prefill(*args, scale=0.1, longest=200)
+    assert out[150:, 1].isnan().all() and lse2[150:, 1].isnan().all()
+    assert torch.isfinite(out[:150, 1]).all() and torch.equal(out[:, 0], want[:, 0]) and torch.equal(lse2[:, 0], lse[:, 0])
 
 
 def test_prefill_strides_and_bounds():
