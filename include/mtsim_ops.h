@@ -161,7 +161,7 @@ size_t sim_op_latent_decode_workspace(int32_t requests, int32_t new_tokens, int3
  * with the rotated key `shared` common to all heads; out and lse as above.
  * Offsets must not decrease; they are bounded by q_rows and k_rows, and at
  * most `longest` queries of a request are computed (`longest` also decides,
- * with the numbers of rows, how the work is tiled, and so the last bits).  Rows that belong to no
+ * with the numbers of rows, requests and heads, how the work is cut, and so the last bits).  Rows that belong to no
  * request are not written.  Types: 16-bit.  Alignment: pointers and strides of
  * q, key, shared, value and out are multiples of 16 bytes; head_dim, key_dim
  * and value_dim are multiples of 8. */

@@ -3,6 +3,7 @@
 #include "tensor.cuh"
 
 #include <cmath>
+#include <cooperative_groups.h>
 #include <cstddef>
 
 namespace mtop {
@@ -49,9 +50,18 @@ struct Args {
     int causal;
     int group;       // heads that run side by side (their keys and values stay in L2)
     int row_blocks;  // of a block's queries
+    int split;       // blocks that share queries
     float scale_log2;  // |scale| log2(e)
     bool negative;
 };
+
+// Few blocks and many keys: a cluster shares a block's queries, each of its
+// blocks taking a stretch of the keys.  In the end each leaves its sums in
+// shared memory, where Q and the first keys were, and joins a share of the rows.
+constexpr int kMostSplit = 8;
+constexpr int kSumsRow = SIM_OP_MAX_HEAD + 4;  // floats, so that eight rows lie in different banks
+constexpr int kStatsOffset = 2 * kRows * kSumsRow * 4;
+static_assert(kStatsOffset + 2 * kRows * 8 <= 6 * kQBytes + kSlots * Shape<2>::slot_bytes, "the sums fit where Q and the ring were");
 
 constexpr int kInFlight = 4;  // tiles of K (and of V) in the ring: a tile of each takes 2 slots or more
 struct Barriers {
@@ -60,7 +70,7 @@ struct Barriers {
     uint32_t tmem;
 };
 
-template <typename T, int TILES>
+template <typename T, int TILES, bool SPLIT>
 __global__ void __launch_bounds__(Shape<TILES>::threads, 3 - TILES)
 k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_q, const __grid_constant__ CUtensorMap m_qr,
           const __grid_constant__ CUtensorMap m_k, const __grid_constant__ CUtensorMap m_kr,
@@ -75,7 +85,8 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     let_next_start();
     after_previous();
     // which rows: within a group of heads the last (longest) row blocks come first
-    int item = blockIdx.x;
+    int item = SPLIT ? blockIdx.x / a.split : blockIdx.x;
+    const int rank = SPLIT ? blockIdx.x % a.split : 0;
     const int per_request = a.row_blocks * a.heads;
     const int b = item / per_request;
     item -= b * per_request;
@@ -83,18 +94,26 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     item -= g0 * a.row_blocks;
     const int h = g0 + item % in_group, base = (a.row_blocks - 1 - item / in_group) * TILES * kRows;
     const int q0 = min(max(a.q_offsets[b], 0), a.q_rows), q1 = min(a.q_offsets[b + 1], a.q_rows);
-    const int k0 = min(max(a.k_offsets[b], 0), a.k_rows), k1 = min(a.k_offsets[b + 1], a.k_rows);
-    const int nq = q1 - q0, nk = max(k1 - k0, 0), rows = min(nq, a.longest);
+    int k0 = min(max(a.k_offsets[b], 0), a.k_rows);
+    const int k1 = min(a.k_offsets[b + 1], a.k_rows);
+    const int nq = q1 - q0, rows = min(nq, a.longest);
+    int nk = max(k1 - k0, 0), behind = nk - nq;  // the first query sees `behind` + 1 keys
     if (base >= rows) return;
     const int start0 = base, start1 = base + kRows;
     auto tiles_for = [&](int start) {  // of keys, for the rows from `start` on
         if (start >= rows) return 0;
-        const int sees = a.causal ? min(nk, min(start + kRows, rows) + nk - nq) : nk;
+        const int sees = a.causal ? min(nk, min(start + kRows, rows) + behind) : nk;
         return sees > 0 ? (sees + kKeys - 1) / kKeys : 0;
     };
-    const int n0 = tiles_for(start0), n1 = TILES == 2 ? tiles_for(start1) : 0, n = max(n0, n1);
+    int n0 = tiles_for(start0), n1 = TILES == 2 ? tiles_for(start1) : 0;
+    if (SPLIT) {  // from here on, of this block's stretch of the keys
+        const int share = (max(n0, n1) + a.split - 1) / a.split, first = rank * share;
+        n0 = min(max(n0 - first, 0), share), n1 = min(max(n1 - first, 0), share);
+        k0 += first * kKeys, nk -= first * kKeys, behind -= first * kKeys;
+    }
+    const int n = max(n0, n1);
     const int qk_blocks = a.head_blocks + a.key_blocks, per_tile = qk_blocks + a.value_blocks;
-    const bool cut = n * kKeys > nk;  // the last tile has rows that are not the request's
+    const bool cut = n > 0 && n * kKeys > nk;  // the last tile has rows that are not the request's
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     bool dead = false;
@@ -258,13 +277,18 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             }
             bar_wait(bar + offsetof(Barriers, v_empty) + ((n - 1) & 3) * 8, ((n - 1) >> 2) & 1, dead);  // every arrival has come
         }
+        if (SPLIT) {
+            __syncwarp();
+            cluster_sync();
+            cluster_sync();
+        }
     } else {
         if (TILES == 2) registers_up<kSoftRegs>();
         // ------------------------------------------------- weights and sums
         const int t = warp / 4, row = (t ? start1 : start0) + (warp % 4) * 32 + lane;
         const int nt = t ? n1 : n0;
-        const int sees = a.causal ? min(nk, row + nk - nq + 1) : nk;  // keys [0, sees) of this row
-        const int first_sees = a.causal ? min(nk, row - lane + nk - nq + 1) : nk;  // of the warp's first row: the fewest
+        const int sees = a.causal ? min(nk, row + behind + 1) : nk;  // keys [0, sees) of this row
+        const int first_sees = a.causal ? min(nk, row - lane + behind + 1) : nk;  // of the warp's first row: the fewest
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
         const uint32_t s_at = tmem + Z::col_s + t * kRows + lanes, o_at = tmem + Z::col_o + t * kRows + lanes;
         const float scale = a.scale_log2;
@@ -331,33 +355,100 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             bar_arrive(smem_addr(&bars->p_ready[t]));
             sum += (s0 + s1) + (s2 + s3);
         }
-        // a sum of 0 is a row that sees nothing: zeros; a sum that is no number stays one
-        if (row < rows && a.lse)
-            a.lse[(int64_t)(q0 + row) * a.heads + h] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
-        const float inv = sum != 0.f ? 1.f / sum : 0.f;
-        T *out = (T *)a.out + (int64_t)(q0 + row) * a.out_row + h * a.out_head;
-        if (nt > 0) {
-            bar_wait(smem_addr(&bars->o_ready[t]), 0, dead);
+        if (SPLIT) {
+            // every product has read what the sums overwrite
+            if (n0 > 0) bar_wait(smem_addr(&bars->o_ready[0]), 0, dead);
+            if (n1 > 0) bar_wait(smem_addr(&bars->o_ready[1]), 0, dead);
             tmem_after_sync();
-        }
+            const int local = t * kRows + (warp % 4) * 32 + lane;
+            ((float2 *)(smem + kStatsOffset))[local] = make_float2(top, sum);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            if (32 * c < 64 * a.value_blocks) {
-                uint32_t o[32];
-                if (nt > 0) {
+            for (int c = 0; c < 4; ++c) {
+                if (32 * c < 64 * a.value_blocks && nt > 0) {
+                    uint32_t o[32];
                     tmem_ld32(o_at + 32 * c, o);
                     tmem_wait_ld();
-                }
-                if (row < rows) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8)
-                        if (32 * c + e < a.value_dim) {
-                            uint4 w;
-                            auto val = [&](int j) { return sum != 0.f ? __uint_as_float(o[e + j]) * inv : 0.f; };
-                            w.x = pack2<T>(val(0), val(1)), w.y = pack2<T>(val(2), val(3));
-                            w.z = pack2<T>(val(4), val(5)), w.w = pack2<T>(val(6), val(7));
-                            *(uint4 *)(out + 32 * c + e) = w;
-                        }
+                    for (int e = 0; e < 32; e += 4)
+                        *(uint4 *)(smem + ((size_t)local * kSumsRow + 32 * c + e) * 4) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                }
+            }
+            __syncwarp();
+            cluster_sync();
+            // A warp takes four rows at a time: lane 8 j + k has the factor of block
+            // k's sums of row j, then each lane four elements of all four rows.
+            const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+            const int there = min(TILES * kRows, rows - base), k8 = lane % kMostSplit;
+            for (int r0 = rank + a.split * 4 * warp; r0 < there; r0 += a.split * 4 * kSoftWarps) {
+                const int mine = r0 + a.split * (lane / kMostSplit);
+                float2 st = make_float2(-INFINITY, 0.f);
+                if (k8 < a.split && mine < there) st = ((const float2 *)cluster.map_shared_rank(smem + kStatsOffset, k8))[mine];
+                float top = st.x;
+#pragma unroll
+                for (int o = kMostSplit / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+                // sums of 0 count as nothing (they may not have been written)
+                const float f = st.y == 0.f ? 0.f : exp2_fast(st.x - (top == -INFINITY ? 0.f : top));
+                const unsigned some = __ballot_sync(~0u, st.y != 0.f);
+                float sum = st.y == 0.f ? 0.f : f * st.y;
+#pragma unroll
+                for (int o = kMostSplit / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+                float4 v[4] = {};
+#pragma unroll 2
+                for (int k = 0; k < a.split; ++k) {
+                    const char *at = (const char *)cluster.map_shared_rank(smem, k) + (r0 * kSumsRow + 4 * lane) * 4;
+                    float4 u[4] = {};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (some >> (kMostSplit * j + k) & 1) u[j] = *(const float4 *)(at + j * a.split * kSumsRow * 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float w = __shfl_sync(~0u, f, kMostSplit * j + k);
+                        v[j].x = fmaf(w, u[j].x, v[j].x), v[j].y = fmaf(w, u[j].y, v[j].y);
+                        v[j].z = fmaf(w, u[j].z, v[j].z), v[j].w = fmaf(w, u[j].w, v[j].w);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float all = __shfl_sync(~0u, sum, kMostSplit * j), inv = all != 0.f ? 1.f / all : 0.f;
+                    const int r = r0 + j * a.split;
+                    if (r < there && 4 * lane < a.value_dim)
+                        *(uint2 *)((T *)a.out + (int64_t)(q0 + base + r) * a.out_row + h * a.out_head + 4 * lane) =
+                            make_uint2(pack2<T>(v[j].x * inv, v[j].y * inv), pack2<T>(v[j].z * inv, v[j].w * inv));
+                }
+                if (a.lse && k8 == 0 && mine < there)
+                    a.lse[(int64_t)(q0 + base + mine) * a.heads + h] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+            }
+            __syncwarp();
+            cluster_sync();  // the others have read
+        } else {
+            // a sum of 0 is a row that sees nothing: zeros; a sum that is no number stays one
+            if (row < rows && a.lse)
+                a.lse[(int64_t)(q0 + row) * a.heads + h] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+            const float inv = sum != 0.f ? 1.f / sum : 0.f;
+            T *out = (T *)a.out + (int64_t)(q0 + row) * a.out_row + h * a.out_head;
+            if (nt > 0) {
+                bar_wait(smem_addr(&bars->o_ready[t]), 0, dead);
+                tmem_after_sync();
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (32 * c < 64 * a.value_blocks) {
+                    uint32_t o[32];
+                    if (nt > 0) {
+                        tmem_ld32(o_at + 32 * c, o);
+                        tmem_wait_ld();
+                    }
+                    if (row < rows) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8)
+                            if (32 * c + e < a.value_dim) {
+                                uint4 w;
+                                auto val = [&](int j) { return sum != 0.f ? __uint_as_float(o[e + j]) * inv : 0.f; };
+                                w.x = pack2<T>(val(0), val(1)), w.y = pack2<T>(val(2), val(3));
+                                w.z = pack2<T>(val(4), val(5)), w.w = pack2<T>(val(6), val(7));
+                                *(uint4 *)(out + 32 * c + e) = w;
+                            }
+                    }
                 }
             }
         }
@@ -368,11 +459,11 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     if (warp == kSoftWarps) tmem_free(tmem, Z::cols);
 }
 
-template <typename T, int TILES>
+template <typename T, int TILES, bool SPLIT>
 int run(const Args &k, const CUtensorMap *m, unsigned grid, cudaStream_t st) {
     static std::atomic<uint64_t> told;
-    if (!allow_shared((const void *)k_prefill<T, TILES>, Shape<TILES>::shared, told)) return SIM_ERR_CUDA;
-    const cudaError_t e = launch_early(k_prefill<T, TILES>, grid, Shape<TILES>::threads, Shape<TILES>::shared, 1, st, k, m[0], m[1], m[2], m[3], m[4]);
+    if (!allow_shared((const void *)k_prefill<T, TILES, SPLIT>, Shape<TILES>::shared, told)) return SIM_ERR_CUDA;
+    const cudaError_t e = launch_early(k_prefill<T, TILES, SPLIT>, grid, Shape<TILES>::threads, Shape<TILES>::shared, k.split, st, k, m[0], m[1], m[2], m[3], m[4]);
     return launched("sim_op_latent_prefill", e);
 }
 
@@ -430,7 +521,23 @@ extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *str
     const int64_t fit = head_bytes > 0 ? (40 << 20) / head_bytes : a->heads;
     const int64_t groups = fit < 1 ? a->heads : (a->heads + fit - 1) / fit;
     k.group = (int)((a->heads + groups - 1) / groups);  // of equal size: a last group of few heads would leave a long tail
-    const int64_t grid = (int64_t)a->requests * k.row_blocks * a->heads;
+    // Keys are split where blocks would leave half of the SMs empty, by as much as
+    // keeps all blocks resident (of clusters of 8 there is room for fewer than 16).
+    // 16 heads of 1,000 queries after 2,728 cached tokens: 50.4 us, two stretches 35.8
+    // (four 45.5); 16 heads of 200 after 1,033: 21.4, two 19.2, four 16.0 (eight 28.0); 4 x
+    // 2,048: 29.4, four 18.2; 4 heads of 200 after 1,100: 22.0, four 15.1, eight 14.8.  The
+    // join takes 3 to 5 us, most where two blocks do it: 16 x 1,024 queries alone 18.4, two 18.6;
+    // 16 heads of 200 after 216: 12.2, four 12.0; after 97: 10.9, four 11.8.
+    const int sms = sm_count();
+    if (!sms) return SIM_ERR_CUDA;
+    k.split = 1;
+    if (tiles == 2) {
+        const int64_t some = a->q_rows / (2 * kRows) + a->requests, most = (int64_t)a->requests * k.row_blocks;
+        const int64_t blocks = (some < most ? some : most) * a->heads;
+        k.split = blocks * 8 <= sms / 2 ? 8 : blocks * 4 <= sms ? 4 : blocks * 2 <= sms ? 2 : 1;
+        if (a->k_rows < (int64_t)a->requests * (k.split == 2 ? 1280 : 448)) k.split = 1;
+    }
+    const int64_t grid = (int64_t)a->requests * k.row_blocks * a->heads * k.split;
     if (grid > INT32_MAX) return fail(SIM_ERR_ARG, "requests * heads * longest is too large");
 
     CUtensorMap m[5];
@@ -458,6 +565,7 @@ extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *str
     if (!ok) return SIM_ERR_CUDA;
     const cudaStream_t st = (cudaStream_t)stream;
     const unsigned g = (unsigned)grid;
-    if (tiles == 1) return bf ? run<__nv_bfloat16, 1>(k, m, g, st) : run<__half, 1>(k, m, g, st);
-    return bf ? run<__nv_bfloat16, 2>(k, m, g, st) : run<__half, 2>(k, m, g, st);
+    if (tiles == 1) return bf ? run<__nv_bfloat16, 1, false>(k, m, g, st) : run<__half, 1, false>(k, m, g, st);
+    if (k.split > 1) return bf ? run<__nv_bfloat16, 2, true>(k, m, g, st) : run<__half, 2, true>(k, m, g, st);
+    return bf ? run<__nv_bfloat16, 2, false>(k, m, g, st) : run<__half, 2, false>(k, m, g, st);
 }

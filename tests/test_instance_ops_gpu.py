@@ -404,6 +404,24 @@ def test_prefill(nq, nk, heads, head, rot, value, dtype, causal):
     check_prefill(*args, scale, *ops.latent_prefill(*args, scale=scale, longest=max(nq) + 1000, causal=causal), causal)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("nq,nk,heads,head,rot,value", [
+    ([1], [9000], 1, 128, 64, 128), ([300, 1, 17, 256], [5000, 2000, 40, 256], 1, 128, 64, 128), ([4000], [4000], 1, 64, 64, 64),
+    ([513, 513], [1300, 3001], 3, 72, 40, 104), ([700, 0], [600, 5000], 2, 128, 64, 8), ([257], [8192], 8, 128, 0, 128)])
+def test_prefill_keys_shared_by_blocks(nq, nk, heads, head, rot, value, dtype, causal):
+    """Few queries and many keys, where blocks take stretches of the keys and join their sums."""
+    args = prefill_case(nq, nk, heads, head, rot, value, dtype, seed=sum(nk))
+    args[1][nk[0] // 3] *= 6  # one block's maximum far above the others'
+    scale = 1.7 / math.sqrt(head + rot)
+    out = torch.full((sum(nq), heads, value), float("nan"), device="cuda", dtype=dtype)
+    lse = torch.full((sum(nq), heads), float("nan"), device="cuda")
+    ops.latent_prefill(*args, scale=scale, longest=max(nq), causal=causal, out=out, lse=lse)
+    check_prefill(*args, scale, out, lse, causal)
+    again, lse2 = ops.latent_prefill(*args, scale=scale, longest=max(nq), causal=causal)
+    assert torch.equal(again, out) and torch.equal(lse2, lse)  # the same bits
+
+
 def test_prefill_requests_do_not_reach_each_other():
     """NaN and infinities in one request's keys and values, and in rows past the last offset, leave the others' rows untouched."""
     nq = nk = [70, 33, 150]
