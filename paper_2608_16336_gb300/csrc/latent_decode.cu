@@ -22,6 +22,11 @@ namespace {
 // (blocks of the same part and different rows run side by side, so that the
 // second finds the cache rows in L2).  A part may begin and end inside
 // a request: such pieces leave their sums in the workspace and k_join adds them.
+//
+// Bound by memory with one row tile: 3 requests of 90,001 to 130,000 tokens (406 MB)
+// take 91.6 us, 4.4 TB/s, of which 20 us are start, end and join.  Bound by the
+// chain from scores to sums with more: 64 requests of 200 to 10,240 tokens, 128
+// heads take 104 us, 480 TFLOP/s (218 MB of cache would take 33 us to read).
 constexpr int kRows = 64;
 constexpr int kRowBlockBytes = kRows * 128;  // 64 rows of 64 elements
 constexpr int kMaxBlocks = 9;                // 64-element column blocks of a row
@@ -631,11 +636,13 @@ template <typename T> int run(const Args &k, const CUtensorMap &m_cache, const C
     if (!allow_shared((const void *)kernel, kShared, told[k.tile == 32])) return SIM_ERR_CUDA;
     cudaError_t e = launch_early(kernel, c.row_tiles * c.lanes, kThreads, kShared, k.pair ? 2 : 1, st, k, m_cache, m_q);
     if (e != cudaSuccess) return launched("sim_op_latent_decode", e);
-    // A row has about lanes / requests pieces: many are shared by a block's
-    // warps, few are one warp's.
-    const bool many = c.lanes > 8 * (int64_t)k.requests;
-    const int64_t rows = (int64_t)k.requests * k.new_tokens * k.heads, per = many ? 1 : kJoinWarps;
-    e = launch_early(many ? k_join<T, kJoinWarps> : k_join<T, 1>, (unsigned)((rows + per - 1) / per), kJoinWarps * 32, 0, 1, st, k);
+    // Few rows: a block shares the pieces of one; many: a warp has a row of its
+    // own.  2 x 128 heads 27.3 us (a warp a row 54.5), 8 x 128 30.4 (44.5), 64 x 16 60.2
+    // (60.8); a warp a row for 16 x 128 heads 48.3 (a block 48.6), 64 x 128 104 (130).
+    const int64_t rows = (int64_t)k.requests * k.new_tokens * k.heads;
+    const bool few = rows <= 1024;
+    const int64_t per = few ? 1 : kJoinWarps;
+    e = launch_early(few ? k_join<T, kJoinWarps> : k_join<T, 1>, (unsigned)((rows + per - 1) / per), kJoinWarps * 32, 0, 1, st, k);
     return launched("sim_op_latent_decode (join)", e);
 }
 
@@ -708,8 +715,9 @@ extern "C" int sim_op_latent_decode(const sim_op_latent_decode_t *a, void *strea
     const uint64_t size[2] = {(uint64_t)k.width, (uint64_t)k.none};
     const int64_t stride[1] = {a->blocks ? a->cache_row : k.width};
     // One row tile: bound by memory, and 5 stages of 32 tokens keep more in
-    // flight than 2 of 64.  More: bound by the tensor core, which takes scores
-    // of 64 tokens in 1,208 cycles and of 32 in 960.
+    // flight than 2 of 64 (3 x 90,001 to 130,000 tokens 91.7 us, with 64 93.7).  More:
+    // bound by the tensor core, which takes scores of 64 tokens in 1,208 cycles and of
+    // 32 in 960 (64 requests, 128 heads 104.2 us, with 32 105.8).
     k.tile = c.row_tiles == 1 ? 32 : 64;
     const int64_t most_rows = (int64_t)a->new_tokens * a->heads;
     k.q_pad = most_rows <= 16 ? 16 : most_rows <= 32 ? 32 : kRows;

@@ -16,7 +16,9 @@ namespace {
 //   O_t += P_t V           (tensor core, P read from tensor memory)
 // The tensor core alternates between the tiles, so that one tile's
 // exponentials overlap the other's products.  K and V pass through a ring of
-// 16 KB slots (128 rows of 64 elements) filled by bulk copies.
+// 16 KB slots (128 rows of 64 elements) filled by bulk copies.  Bound by the
+// tensor core and the thread that feeds it: a prompt of 8,192 tokens, 64 heads
+// takes 820 to 880 us, 1.56 to 1.68 PFLOP/s.
 constexpr int kRows = 128;              // of a tile of queries
 constexpr int kQBytes = kRows * 128;    // of one column block (64 elements)
 constexpr int kSlots = 8;
@@ -88,7 +90,7 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     // row blocks of all requests first: 6 x 2,534 queries, 3 heads 35.8 us (a request
     // after another 42.8).  With one tile, where many row blocks are empty and the
     // blocks short (a division more shows), a request after another: 37 ragged
-    // prompts up to 300 23.8 us (25.5).
+    // prompts up to 300 23.2 us (25.5).
     int item = SPLIT ? blockIdx.x / a.split : blockIdx.x;
     const int rank = SPLIT ? blockIdx.x % a.split : 0;
     int g0 = 0, in_group = a.heads;
@@ -518,9 +520,9 @@ extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *str
     k.negative = a->scale < 0;
     const int64_t longest = a->longest < a->q_rows ? a->longest : a->q_rows;
     // One tile a block where most prompts leave the second one empty and keys
-    // are few: 37 ragged prompts up to 300, 16 heads 26.7 us (two tiles 34.8), 64 x 128
-    // tokens, 64 heads 134 us (189); two tiles for the rest: 37 x 512 tokens 98.8 us (one
-    // 117), 16 x 256 tokens after up to 1,000 cached ones 77 us (95).
+    // are few: 37 ragged prompts up to 300, 16 heads 23.2 us (two tiles 31.1), 64 x 128
+    // tokens, 64 heads 129 us (189); two tiles for the rest: 37 x 512 tokens 98.8 us (one
+    // 113), 16 x 256 tokens after up to 1,000 cached ones 76 us (91).
     const int tiles = longest <= 384 && a->q_rows <= 192 * (int64_t)a->requests && a->k_rows <= 384 * (int64_t)a->requests ? 1 : 2;
     k.row_blocks = (int)((longest + tiles * kRows - 1) / (tiles * kRows));
     // Heads side by side: as many as keep their keys and values within about a third of L2.

@@ -13,6 +13,8 @@ typedef unsigned long long u64;
 // A row belongs to a cluster of 1 to 8 blocks, each of which holds a part of it
 // in shared memory, so that the row is read from memory once however many
 // passes the limits take; sums and histograms meet in distributed shared memory.
+// Bound by instructions (22 a logit) and a chain of a dozen cluster barriers, not
+// by memory: 64 x 131,075 bfloat16 take 43 us (17 MB), 1 x 32,000 floats 15.5 us.
 //
 // Weights are whole numbers of 2^-40: their sums are exact, so neither the
 // order of the additions nor the split over threads and blocks changes a
@@ -819,9 +821,10 @@ template <typename T> int run(const sim_op_sample_t *a, cudaStream_t st) {
     const int sms = sm_count();
     if (!sms) return SIM_ERR_CUDA;
     // Blocks a row: so many that two blocks' parts fit in a multiprocessor's shared
-    // memory (128 x 131,075 bfloat16: 4 blocks 86 us, 2 blocks 101), and more while all
+    // memory (128 x 131,075 bfloat16: 4 blocks 81 us, 2 blocks 92), and more while all
     // rows' blocks still run at once and a part is 2,048 logits or more (64 rows of
-    // that: 4 blocks 45 us, 8 blocks 65; 1 x 32,000: 8 blocks 21 us, 2 blocks 25).
+    // that: 4 blocks 43 us, 8 blocks 62; 64 x 32,000: 4 blocks 26 us, 1 block 45; 64 x
+    // 8,000: 2 blocks 22.5 us, 4 blocks 23.1; 1 x 32,000: 8 blocks 16 us, 2 blocks 21).
     constexpr int N = 16 / sizeof(T);
     int blocks = 1;
     auto stretch = [&](int n) { return (int)(((int64_t)a->vocab + N - 1 + (int64_t)n * kWarps * 32 * N - 1) / ((int64_t)n * kWarps * 32 * N)) * 32 * N; };
