@@ -13,8 +13,8 @@ typedef unsigned long long u64;
 // A row belongs to a cluster of 1 to 8 blocks, each of which holds a part of it
 // in shared memory, so that the row is read from memory once however many
 // passes the limits take; sums and histograms meet in distributed shared memory.
-// Bound by instructions (22 a logit) and a chain of a dozen cluster barriers, not
-// by memory: 64 x 131,075 bfloat16 take 43 us (17 MB), 1 x 32,000 floats 15.5 us.
+// Bound by instructions (about 20 a logit) and a chain of a dozen cluster barriers,
+// not by memory: 64 x 131,075 bfloat16 take 39.5 us (17 MB), 1 x 32,000 floats 16 us.
 //
 // Weights are whole numbers of 2^-40: their sums are exact, so neither the
 // order of the additions nor the split over threads and blocks changes a
@@ -50,7 +50,7 @@ __device__ __forceinline__ float exp2_near(float x) {
 struct Cut {
     uint32_t hi, lo;
     __device__ __forceinline__ explicit Cut(float x) {
-        const float t = __fadd_rz(x * 3.814697265625e-06f, 8388608.f);
+        const float t = __fmaf_rz(x, 3.814697265625e-06f, 8388608.f);
         hi = __float_as_uint(t), lo = __float_as_uint(fmaf(t - 8388608.f, -262144.f, x) + 8388608.f);
     }
     __device__ __forceinline__ u64 units() const { return ((u64)(hi - 0x4B000000u) << 18) + (lo - 0x4B000000u); }
@@ -469,25 +469,38 @@ template <typename T> __global__ void __launch_bounds__(kThreads, 2) k_sample(co
                 const uint32_t at = atomicAdd(&sh.listed[l], 1u);
                 if (at < kList) sh.list[l][at] = key_of(v), sh.place[l][at] = pos;
             };
-            part.each([&](int pos, const float *v) {
+            if (limit_k) {
+                // What is below all candidates adds to nothing: most steps of a warp skip
+                // the rest (64 x 131,075, k = 1,000 32.5 us; without 36.4).
+                const float lowest = limit_p ? fminf(low_k, low_p) : low_k;
+                part.each([&](int pos, const float *v) {
 #pragma unroll
-                for (int e = 0; e < Part<T>::N; ++e) {
-                    const Cut x(w.of(v[e]));
-                    if (limit_k) {
+                    for (int e = 0; e < Part<T>::N; ++e) {
+                        if (!__any_sync(~0u, v[e] >= lowest)) continue;
+                        const Cut x(w.of(v[e]));
                         const bool above = v[e] > top_k;
                         m1.add_if(above, x);
                         count += above;
                         if (!above && v[e] >= low_k) list(0, v[e], pos + e);
-                    } else {
-                        m1.add(x);
+                        if (limit_p) {
+                            const bool above_p = v[e] > top_p;
+                            m2.add_if(above_p, x);
+                            if (!above_p && v[e] >= low_p) list(1, v[e], pos + e);
+                        }
                     }
-                    if (limit_p) {
+                });
+            } else {
+                part.each([&](int pos, const float *v) {
+#pragma unroll
+                    for (int e = 0; e < Part<T>::N; ++e) {
+                        const Cut x(w.of(v[e]));
                         const bool above = v[e] > top_p;
+                        m1.add(x);
                         m2.add_if(above, x);
                         if (!above && v[e] >= low_p) list(1, v[e], pos + e);
                     }
-                }
-            });
+                });
+            }
             total_of(m1.units(), m2.units(), count, over, nullptr);
             if (threadIdx.x < blocks) {
                 const Sums *from = peer(&sh.sums[turn ^ 1], threadIdx.x);
@@ -821,10 +834,10 @@ template <typename T> int run(const sim_op_sample_t *a, cudaStream_t st) {
     const int sms = sm_count();
     if (!sms) return SIM_ERR_CUDA;
     // Blocks a row: so many that two blocks' parts fit in a multiprocessor's shared
-    // memory (128 x 131,075 bfloat16: 4 blocks 81 us, 2 blocks 92), and more while all
+    // memory (128 x 131,075 bfloat16: 4 blocks 75 us, 2 blocks 86), and more while all
     // rows' blocks still run at once and a part is 2,048 logits or more (64 rows of
-    // that: 4 blocks 43 us, 8 blocks 62; 64 x 32,000: 4 blocks 26 us, 1 block 45; 64 x
-    // 8,000: 2 blocks 22.5 us, 4 blocks 23.1; 1 x 32,000: 8 blocks 16 us, 2 blocks 21).
+    // that: 4 blocks 39.5 us, 8 blocks 58; 64 x 32,000: 4 blocks 25.5 us, 1 block 44; 64 x
+    // 8,000: 2 blocks 22.7 us, 4 blocks 23.2; 1 x 32,000: 8 blocks 16 us, 2 blocks 19.5).
     constexpr int N = 16 / sizeof(T);
     int blocks = 1;
     auto stretch = [&](int n) { return (int)(((int64_t)a->vocab + N - 1 + (int64_t)n * kWarps * 32 * N - 1) / ((int64_t)n * kWarps * 32 * N)) * 32 * N; };
