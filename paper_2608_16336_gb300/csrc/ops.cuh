@@ -110,9 +110,6 @@ __device__ __forceinline__ void angle_cos_sin(unsigned long long turns, long lon
     sincospif((float)(int)(at >> 32) * 4.656612873077393e-10f /* 2^-31: half turns */, &s, &c);
 }
 
-// Barrier `id` of the block's first (or other) `threads` threads.
-__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-
 // The kernels before this one in the stream have ended and what they wrote is
 // visible; the one after it may start (and wait here) from now on.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;"); }

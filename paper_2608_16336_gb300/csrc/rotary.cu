@@ -73,72 +73,89 @@ template <typename T, bool HALF> __device__ __forceinline__ void turn_pairs(Vec<
 }
 
 // The tensors' vectors are aligned and the rotated part is made of whole ones:
-// bound by memory.  A block takes a token at a time: its first warps rotate,
-// with the token's cosines and sines (computed once, in shared memory) of their
-// one vector of a head in registers over all the heads they take; the other
-// warps copy the rest of the heads.  (One loop for both made every warp issue
-// both: 225 us instead of 128 for 8,192 x 128 heads of 192 with 64 rotated, 805 MB.)
-constexpr int kRotaryWarps = 8;
+// bound by memory.  A block takes a group of tokens at a time, computes all their
+// cosines and sines in shared memory, and its threads take vectors (pairs of them
+// in the half layout) of any token and head: first all that rotate, then all that are copied,
+// so that no warp does both.  8,192 tokens x 128 heads of 192 with 64 rotated
+// (805 MB) take 122 to 125 us, 6.5 TB/s; 13,850 x 12 heads of 104 (69 MB) 15 us; 11,407
+// tokens of 32 floats 6 us.
+constexpr int kGroupThreads = 256, kGroupBlocks = 4, kGroupTurns = 1024, kGroupVectors = 2048;
+
+// u / d for u, d < 2^16 (d = 0: there is no u)
+struct Divider {
+    uint32_t d, m;
+    __host__ explicit Divider(uint32_t by) : d(by), m(by > 1 ? (uint32_t)(((1ull << 32) + by - 1) / by) : 0) {}
+    __device__ __forceinline__ uint32_t operator()(uint32_t u) const { return d == 1 ? u : __umulhi(u, m); }
+};
+struct Group {
+    int tokens;
+    Divider turned_token, turned_head, rest_token, rest_head;  // vectors of a token and of a head
+};
 
 template <typename T, bool HALF>
-__global__ void __launch_bounds__(kRotaryWarps * 32) k_rotary_wide(const __grid_constant__ sim_op_rotary_t a, int turn_warps) {
-    constexpr int N = Vec<T>::N, P = HALF ? N : N / 2;  // pairs of a thread
-    __shared__ float2 turn[SIM_OP_MAX_ROT / 2];
-    const int half = a.rot_dim / 2, turned = a.rot_dim / N / (HALF ? 2 : 1), rest = (a.dim - a.rot_dim) / N;
+__global__ void __launch_bounds__(kGroupThreads, kGroupBlocks) k_rotary_wide(const __grid_constant__ sim_op_rotary_t a, const __grid_constant__ Group g) {
+    constexpr int N = Vec<T>::N, P = HALF ? N : N / 2;
+    __shared__ __align__(16) float2 turn[kGroupTurns];
+    __shared__ unsigned long long per[SIM_OP_MAX_ROT / 2];
+    const int half = a.rot_dim / 2;
     let_next_start();
     after_previous();
-    const bool turns = (int)threadIdx.x < turn_warps * 32;
-    const int units = turns ? turned : rest, threads = turns ? turn_warps * 32 : (kRotaryWarps - turn_warps) * 32;
-    const int id = turns ? threadIdx.x : threadIdx.x - turn_warps * 32;
-    // this thread's vector of a head, the heads it takes: h0, h0 + step, ..
-    const int step = units ? threads / units : 0, u = units ? id % units : 0, h0 = step && id / units < step ? id / units : a.heads;
-    int at = turns ? a.rot_offset + u * N : u * N;
-    if (!turns && at >= a.rot_offset) at += a.rot_dim;
-    const int64_t x_step = step * a.x_head, y_step = step * a.out_head;
-    unsigned long long per = 0;
-    if (threadIdx.x < half) per = turns_per_position(a.frequencies[threadIdx.x]);
-    for (int64_t n = blockIdx.x; n < a.tokens; n += gridDim.x) {
-        const int64_t p = a.positions_64 ? ((const int64_t *)a.positions)[n] : ((const int32_t *)a.positions)[n];
-        const T *x = (const T *)a.x + n * a.x_token + h0 * a.x_head + at;
-        T *y = (T *)a.out + n * a.out_token + h0 * a.out_head + at;
-        if (!turns) {
-            // loads of several heads before their stores: the compiler cannot tell that heads do not overlap
-            for (int h = h0; h < a.heads; h += 4 * step) {
-                Vec<T> v[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k, x += x_step)
-                    if (h + k * step < a.heads) v[k] = *(const Vec<T> *)x;
-#pragma unroll
-                for (int k = 0; k < 4; ++k, y += y_step)
-                    if (h + k * step < a.heads) *(Vec<T> *)y = v[k];
-            }
-            continue;
-        }
-        named_sync(1, turn_warps * 32);
-        for (int i = threadIdx.x; i < half; i += turn_warps * 32) {
+    if (threadIdx.x < half) per[threadIdx.x] = turns_per_position(a.frequencies[threadIdx.x]);
+    for (int64_t n0 = (int64_t)blockIdx.x * g.tokens; n0 < a.tokens; n0 += (int64_t)gridDim.x * g.tokens) {
+        const uint32_t here = (uint32_t)min((int64_t)g.tokens, a.tokens - n0);
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < here * half; i += kGroupThreads) {
+            const uint32_t tok = i / half;
+            const int64_t n = n0 + tok, p = a.positions_64 ? ((const int64_t *)a.positions)[n] : ((const int32_t *)a.positions)[n];
             float c, s;
-            angle_cos_sin(i == threadIdx.x ? per : turns_per_position(a.frequencies[i]), a.inverse ? -p : p, c, s);
+            angle_cos_sin(per[i - tok * half], a.inverse ? -p : p, c, s);
             turn[i] = make_float2(c * a.amplitude, s * a.amplitude);
         }
-        named_sync(1, turn_warps * 32);
-        float2 t[P];
-#pragma unroll
-        for (int i = 0; i < P; ++i) t[i] = turn[u * P + i];
-        for (int h = h0; h < a.heads; h += 2 * step) {
+        __syncthreads();
+        const T *x = (const T *)a.x + n0 * a.x_token;
+        T *y = (T *)a.out + n0 * a.out_token;
+        // loads of two vectors (or pairs of vectors) before their stores
+        const uint32_t turned = here * g.turned_token.d, rest = a.x == a.out ? 0 : here * g.rest_token.d;
+        for (uint32_t u0 = threadIdx.x; u0 < turned; u0 += 2 * kGroupThreads) {
             Vec<T> v[2], w[2];
+            int64_t to[2];
+            uint32_t t_at[2];
 #pragma unroll
-            for (int k = 0; k < 2; ++k, x += x_step)
-                if (h + k * step < a.heads) {
-                    v[k] = *(const Vec<T> *)x;
-                    if (HALF) w[k] = *(const Vec<T> *)(x + half);
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t u = u0 + k * kGroupThreads;
+                if (u < turned) {
+                    const uint32_t tok = g.turned_token(u), r = u - tok * g.turned_token.d, h = g.turned_head(r), j = r - h * g.turned_head.d;
+                    const T *from = x + tok * a.x_token + h * a.x_head + a.rot_offset + j * N;
+                    v[k] = *(const Vec<T> *)from;
+                    if (HALF) w[k] = *(const Vec<T> *)(from + half);
+                    to[k] = tok * a.out_token + h * a.out_head + a.rot_offset + j * N, t_at[k] = tok * half + j * P;
                 }
+            }
 #pragma unroll
-            for (int k = 0; k < 2; ++k, y += y_step)
-                if (h + k * step < a.heads) {
-                    turn_pairs<T, HALF>(v[k], w[k], t);
-                    *(Vec<T> *)y = v[k];
-                    if (HALF) *(Vec<T> *)(y + half) = w[k];
+            for (int k = 0; k < 2; ++k)
+                if (u0 + k * kGroupThreads < turned) {
+                    turn_pairs<T, HALF>(v[k], w[k], turn + t_at[k]);
+                    *(Vec<T> *)(y + to[k]) = v[k];
+                    if (HALF) *(Vec<T> *)(y + to[k] + half) = w[k];
                 }
+        }
+        for (uint32_t u0 = threadIdx.x; u0 < rest; u0 += 4 * kGroupThreads) {
+            Vec<T> v[4];
+            int64_t to[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t u = u0 + k * kGroupThreads;
+                if (u < rest) {
+                    const uint32_t tok = g.rest_token(u), r = u - tok * g.rest_token.d, h = g.rest_head(r);
+                    int at = (int)(r - h * g.rest_head.d) * N;
+                    if (at >= a.rot_offset) at += a.rot_dim;
+                    v[k] = *(const Vec<T> *)(x + tok * a.x_token + h * a.x_head + at);
+                    to[k] = tok * a.out_token + h * a.out_head + at;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (u0 + k * kGroupThreads < rest) *(Vec<T> *)(y + to[k]) = v[k];
         }
     }
 }
@@ -235,18 +252,24 @@ bool whole(int n, std::initializer_list<const void *> pointers, std::initializer
     return true;
 }
 
-template <typename T> int run_rotary(const sim_op_rotary_t *a, cudaStream_t st) {
+template <typename T> int run_rotary(const sim_op_rotary_t *a, int sms, cudaStream_t st) {
     constexpr int N = 16 / sizeof(T);
     const bool half = a->layout == SIM_OP_HALF;
     const int turned = a->rot_dim / N / (half ? 2 : 1), rest = (a->dim - a->rot_dim) / N;
-    // warps in proportion to the bytes they move; in place nothing is copied
-    int turn_warps = a->x == a->out || rest == 0 ? kRotaryWarps : (kRotaryWarps * a->rot_dim + a->dim / 2) / a->dim;
-    turn_warps = turn_warps < 1 ? 1 : turn_warps > kRotaryWarps - (rest && a->x != a->out) ? kRotaryWarps - (rest && a->x != a->out) : turn_warps;
+    const int64_t most = (int64_t)a->heads * (turned > rest ? turned : rest);  // vectors of a token
     cudaError_t e;
-    if (whole(N, {a->x, a->out}, {a->x_token, a->x_head, a->out_token, a->out_head, a->dim, a->rot_offset, half ? a->rot_dim / 2 : a->rot_dim}) &&
-        turned <= 32 * turn_warps && (turn_warps == kRotaryWarps || rest <= 32 * (kRotaryWarps - turn_warps))) {
-        const unsigned grid = (unsigned)(a->tokens < 16384 ? a->tokens : 16384);
-        e = launch_early(half ? k_rotary_wide<T, true> : k_rotary_wide<T, false>, grid, kRotaryWarps * 32, 0, 1, st, *a, turn_warps);
+    if (most < 65536 && whole(N, {a->x, a->out}, {a->x_token, a->x_head, a->out_token, a->out_head, a->dim, a->rot_offset, half ? a->rot_dim / 2 : a->rot_dim})) {
+        // As many tokens as give a thread eight vectors, while every block has a group:
+        // 16,384 tokens, 24 heads of 192 50 to 53 us with 4 to 8 tokens (one 77.5), 12,000 x 8
+        // heads 12 us with 12 (one 30); 8,192 x 128 heads 122 us with one (two 131).
+        int64_t group = a->tokens / (kGroupBlocks * (int64_t)sms);
+        if (group > kGroupVectors / most) group = kGroupVectors / most;
+        if (group > kGroupTurns / (a->rot_dim / 2)) group = kGroupTurns / (a->rot_dim / 2);
+        if (group < 1) group = 1;
+        const Group g = {(int)group, Divider(a->heads * turned), Divider(turned), Divider(a->heads * rest), Divider(rest)};
+        const int64_t groups = (a->tokens + group - 1) / group, blocks = kGroupBlocks * (int64_t)sms;
+        const unsigned grid = (unsigned)(groups < blocks ? groups : blocks);
+        e = launch_early(half ? k_rotary_wide<T, true> : k_rotary_wide<T, false>, grid, kGroupThreads, 0, 1, st, *a, g);
     } else {
         e = launch_early(k_rotary<T>, (unsigned)(a->tokens < (1 << 20) ? a->tokens : (1 << 20)), 256, 0, 1, st, *a);
     }
@@ -287,9 +310,11 @@ extern "C" int sim_op_rotary(const sim_op_rotary_t *a, void *stream) {
     if (!a->x || !a->out || !a->positions || !a->frequencies) return fail(SIM_ERR_ARG, "x, out, positions and frequencies must not be NULL");
     if (a->x == a->out && (a->x_token != a->out_token || a->x_head != a->out_head))
         return fail(SIM_ERR_ARG, "in place, out must have x's strides");
+    const int sms = sm_count();
+    if (!sms) return SIM_ERR_CUDA;
     const cudaStream_t st = (cudaStream_t)stream;
-    if (a->type == SIM_OP_BF16) return run_rotary<__nv_bfloat16>(a, st);
-    return a->type == SIM_OP_FP16 ? run_rotary<__half>(a, st) : run_rotary<float>(a, st);
+    if (a->type == SIM_OP_BF16) return run_rotary<__nv_bfloat16>(a, sms, st);
+    return a->type == SIM_OP_FP16 ? run_rotary<__half>(a, sms, st) : run_rotary<float>(a, sms, st);
 }
 
 extern "C" int sim_op_latent_append(const sim_op_latent_append_t *a, void *stream) {

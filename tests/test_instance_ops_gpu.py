@@ -82,6 +82,25 @@ def test_rotary(tokens, heads, dim, rot, offset, dtype, layout):
 
 
 @pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("tokens,heads,dim,rot,offset", [(20011, 1, 32, 32, 0), (3001, 12, 104, 96, 8), (5000, 10, 160, 32, 64), (2500, 1, 512, 256, 0),
+                                                         (1300, 300, 64, 32, 16)])
+def test_rotary_many_tokens(tokens, heads, dim, rot, offset, dtype, layout):
+    """Groups of tokens a block, the last one short; nothing past the last token is written."""
+    g = gen(tokens)
+    x = randn(g, tokens, heads, dim, dtype=dtype)
+    pos = torch.randint(0, 100000, (tokens,), generator=g, device="cuda")
+    f = ops.rotary_frequencies(rot)
+    store = torch.full((tokens + 3, heads, dim), 7.0, device="cuda", dtype=dtype)
+    y = ops.rotary(x, pos, f, layout=layout, offset=offset, out=store[:tokens])
+    check_rotary(x, pos, f, y, layout, offset)
+    assert (store[tokens:] == 7.0).all()
+    store[:tokens] = x
+    ops.rotary(store[:tokens], pos, f, layout=layout, offset=offset, out=store[:tokens])
+    assert torch.equal(store[:tokens], ops.rotary(x, pos, f, layout=layout, offset=offset)) and (store[tokens:] == 7.0).all()
+
+
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
 def test_rotary_positions_far_out(layout):
     g = gen(1)
     pos = torch.tensor([0, 1, -1, 2 ** 31 - 1, -2 ** 31, 2 ** 40 + 12345, -2 ** 62, 10 ** 15, 7], device="cuda")
