@@ -714,15 +714,16 @@ extern "C" int sim_op_latent_decode(const sim_op_latent_decode_t *a, void *strea
     CUtensorMap m, mq;
     const uint64_t size[2] = {(uint64_t)k.width, (uint64_t)k.none};
     const int64_t stride[1] = {a->blocks ? a->cache_row : k.width};
-    // One row tile: bound by memory, and 5 stages of 32 tokens keep more in
-    // flight than 2 of 64 (3 x 90,001 to 130,000 tokens 91.7 us, with 64 93.7).  More:
-    // bound by the tensor core, which takes scores of 64 tokens in 1,208 cycles and of
-    // 32 in 960 (64 requests, 128 heads 104.2 us, with 32 105.8).
-    k.tile = c.row_tiles == 1 ? 32 : 64;
     const int64_t most_rows = (int64_t)a->new_tokens * a->heads;
     k.q_pad = most_rows <= 16 ? 16 : most_rows <= 32 ? 32 : kRows;
     const int col_blocks = (k.width + 63) / 64;
-    k.stages = (kShared - kRowBlockBytes - 1024 - col_blocks * k.q_pad * 128) / (col_blocks * k.tile * 128);
+    auto stages_of = [&](int tile) { return (kShared - kRowBlockBytes - 1024 - col_blocks * k.q_pad * 128) / (col_blocks * tile * 128); };
+    // Tiles of 64 tokens, whose scores take 1,208 cycles (of 32: 960).  Where only two
+    // stages of 64 fit and one row tile leaves time to spare, five of 32 keep more
+    // in flight: 3 x 90,001 to 130,000 tokens, rank 512 91.7 us, with 64 93.7.  Rank 384 70.3 us,
+    // with 32 82.9; rank 256 54.1 (74.2); 64 requests of rank 512, 128 heads 104.2 (105.8).
+    k.tile = c.row_tiles == 1 && stages_of(64) < 3 ? 32 : 64;
+    k.stages = stages_of(k.tile);
     if (k.stages > kMostStages) k.stages = kMostStages;
     k.run = 4;
     while (k.run < k.tile && a->block_tokens % (2 * k.run) == 0) k.run *= 2;
