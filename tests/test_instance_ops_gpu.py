@@ -352,6 +352,36 @@ def test_decode_on_another_stream():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def test_calls_in_a_row_keep_their_order():
+    """Kernels whose blocks are set up early still see all that earlier calls wrote: the same bits as with a wait after every call."""
+    def steps(wait):
+        g = gen(31)
+        q, cache, table, n = decode_case([900, 70, 300], 1, 16, 512, 64, 16, BF, seed=31, junk=0.0)
+        x, pos = randn(g, 3000, 4, 64, dtype=BF), torch.arange(3000, device="cuda")
+        latent, key, at = randn(g, 3, 512, dtype=BF), randn(g, 3, 64, dtype=BF), torch.tensor([5, 9, 2], device="cuda")
+        f, u = ops.rotary_frequencies(64), torch.full((3,), 0.37, device="cuda")
+        rows = torch.arange(3, device="cuda")
+        prompt = prefill_case([200, 90], [700, 90], 2, 64, 64, 64, BF, seed=31)
+        tokens, outs = [], [torch.empty(3, 1, 16, 512, device="cuda", dtype=BF) for _ in range(2)] + [torch.empty(290, 2, 64, device="cuda", dtype=BF)]
+        for i in range(25):
+            slot = table[rows, 2].long() * 16 + i % 16  # a row of the third block, seen by every request
+            for call in (lambda: ops.rotary(x, pos, f, layout="half", out=x), lambda: ops.rotary(x, pos, f, layout="half", inverse=i % 3 == 0, out=x),
+                         lambda: ops.rotary(q[:, 0, :, 512:], at, f, out=q[:, 0, :, 512:]),
+                         lambda: ops.latent_append(latent, key, at, f, slot, cache),
+                         lambda: ops.latent_decode(q, cache, table, n, scale=0.1, out=outs[0]),
+                         lambda: ops.latent_decode(q, cache, table, n, scale=0.3, out=outs[1]),
+                         lambda: ops.rotary(outs[0][:, 0], at, f, out=outs[0][:, 0]), lambda: q[..., :512].copy_(outs[0] + outs[1]),
+                         lambda: ops.rotary(prompt[0], at.new_zeros(290) + i, f, layout="half", offset=64, out=prompt[0]),
+                         lambda: ops.latent_prefill(*prompt, scale=0.2, longest=200, out=outs[2]), lambda: prompt[0][..., :64].copy_(outs[2]),
+                         lambda: tokens.append(ops.sample(q[:, 0].reshape(3, -1), u, top_k=rows.int() + 5)[0])):
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+        return [x, q, cache, prompt[0], torch.stack(tokens)]
+    want = steps(True)
+    assert all(torch.equal(a, b) for _ in range(3) for a, b in zip(steps(False), want))
+
+
 def test_operators_in_a_graph():
     q, cache, table, n = decode_case([600, 1200], 1, 32, 512, 64, 16, BF, seed=8)
     logits, u = torch.randn(2, 5000, device="cuda", generator=gen(1)), torch.tensor([0.3, 0.8], device="cuda")
