@@ -47,6 +47,10 @@ _WORKSPACE: dict[tuple, int] = {}  # bytes by sizes
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
+# Scratch memory of the current device on a stream, without a tensor around it: 5 us less of a small call's 16.
+_scratch = getattr(torch._C, "_cuda_cudaCachingAllocator_raw_alloc", None) or (
+    lambda nbytes, stream: torch.cuda.caching_allocator_alloc(nbytes, stream=stream))
+_release = getattr(torch._C, "_cuda_cudaCachingAllocator_raw_delete", None) or torch.cuda.caching_allocator_delete
 
 
 def lib() -> ctypes.CDLL:
@@ -270,12 +274,16 @@ def latent_decode(q, cache, table, lengths, *, scale, out=None, lse=None):
     nbytes = _WORKSPACE.get(size)
     if nbytes is None:
         nbytes = _WORKSPACE[size] = L.sim_op_latent_decode_workspace(b, new, heads, rank)
-    work = torch.empty(nbytes + 1, dtype=torch.uint8, device=q.device)  # (new_empty takes 2 us longer)
-    rc = L.sim_op_latent_decode(
-        DECODE.pack(q.data_ptr(), cache.data_ptr(), table.data_ptr(), lengths.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                    work.data_ptr(), nbytes, qs[0], qs[1], qs[2], os_[0], os_[1], os_[2], cs[0], cs[1], ts[0], blocks, b, new,
-                    heads, rank, width - rank, block, table.shape[1], code, scale),
-        _stream_of(device))
+    stream = _stream_of(device)
+    work = _scratch(nbytes, stream)
+    try:
+        rc = L.sim_op_latent_decode(
+            DECODE.pack(q.data_ptr(), cache.data_ptr(), table.data_ptr(), lengths.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                        work, nbytes, qs[0], qs[1], qs[2], os_[0], os_[1], os_[2], cs[0], cs[1], ts[0], blocks, b, new,
+                        heads, rank, width - rank, block, table.shape[1], code, scale),
+            stream)
+    finally:
+        _release(work)  # what the stream allocates next comes after this call's kernels
     if rc:
         _failed(rc)
     return out, lse
