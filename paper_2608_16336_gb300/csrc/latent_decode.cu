@@ -64,7 +64,6 @@ struct Args {
     int q_pad;                    // rows of Q kept: 16, 32 or 64
     int run;                      // tokens a copy takes
     bool scattered;               // four rows anywhere instead of a run
-    bool pair;                    // two row tiles of a part share their copies
     bool q_flat;                  // Q's rows are one line to the copies
     int none;                     // a row outside the cache
     float scale_log2;
@@ -136,8 +135,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
     if (warp == 1 && lane == 0) {
         for (int s = 0; s < a.stages; ++s) {
             bar_init(smem_addr(&bars->full[s]), 1);
-            bar_init(smem_addr(&bars->empty[s][0]), a.pair ? 2 : 1);
-            bar_init(smem_addr(&bars->empty[s][1]), a.pair ? 2 : 1);
+            bar_init(smem_addr(&bars->empty[s][0]), 1);
+            bar_init(smem_addr(&bars->empty[s][1]), 1);
         }
         bar_init(smem_addr(&bars->q_full), a.q_flat ? 1 : 64);
         bar_init(smem_addr(&bars->q_empty), 1);
@@ -186,8 +185,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
     }
     __syncwarp();
     tmem_before_sync();
-    if (a.pair) cluster_sync();
-    else __syncthreads();
+    __syncthreads();
     tmem_after_sync();
     const uint32_t tmem = bars->tmem;
     const int parts = parts_of(a, bars->total);
@@ -219,9 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
                 const uint32_t parity = (round & 1) ^ 1, full = smem_addr(&bars->full[s]);
                 const uint32_t dst = stage_at + s * stage_bytes + group * run * 128;
                 auto copy = [&](int c) {
-                    if (a.pair) {  // even column blocks by the first block of the pair, odd ones by the second
-                        if ((c & 1) == (int)(blockIdx.x & 1)) copy_box_2d_pair(dst + c * Z::block_bytes, &m_cache, 64 * c, row[0], full);
-                    } else if (a.scattered) copy_rows_4(dst + c * Z::block_bytes, &m_cache, 64 * c, row[0], row[1], row[2], row[3], full);
+                    if (a.scattered) copy_rows_4(dst + c * Z::block_bytes, &m_cache, 64 * c, row[0], row[1], row[2], row[3], full);
                     else copy_box_2d(dst + c * Z::block_bytes, &m_cache, 64 * c, row[0], full);
                 };
                 bar_wait(smem_addr(&bars->empty[s][0]), parity, dead);
@@ -285,10 +281,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
                 for (int k = 0; k < 4; ++k) product_ss<kHigh, kHigh>(d, q_low + 2 * k, c_low + 2 * k, word_s, c + k > 0);
             product_commit(smem_addr(&bars->s_ready[i % Z::scores]));
         };
-        auto release = [&](uint32_t bar) {
-            if (a.pair) product_commit_pair(bar);
-            else product_commit(bar);
-        };
         auto weighted = [&](int i, int s, bool add) {
             const int w = i % Z::weights;
             const uint32_t w_low = operand_low(p_at + w * (TILE * 2), 16);
@@ -298,9 +290,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
 #pragma unroll
                 for (int e = 0; e < TILE / 16; ++e)
                     product_ss<kHigh, kHigh>(tmem + 64 * c, w_low + 2 * e, c_low + 128 * e, word, add || e > 0);
-                if (c == 0) release(smem_addr(&bars->empty[s][0]));
+                if (c == 0) product_commit(smem_addr(&bars->empty[s][0]));
             }
-            release(smem_addr(&bars->empty[s][1]));
+            product_commit(smem_addr(&bars->empty[s][1]));
             product_commit(smem_addr(&bars->pv_done[w]));
         };
         // Scores run ahead of the weighted sums by as many tiles as there are
@@ -534,8 +526,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
     }
     __syncwarp();
     tmem_before_sync();
-    if (a.pair) cluster_sync();  // the other block's copies and arrivals have come
-    else __syncthreads();
+    __syncthreads();
     if (warp == kSoftWarps) tmem_free(tmem, kCols);
 }
 
@@ -639,7 +630,7 @@ template <typename T> int run(const Args &k, const CUtensorMap &m_cache, const C
     auto kernel = k.tile == 32 ? k_decode<T, 32> : k_decode<T, 64>;
     static std::atomic<uint64_t> told[2];
     if (!allow_shared((const void *)kernel, kShared, told[k.tile == 32])) return SIM_ERR_CUDA;
-    cudaError_t e = launch_early(kernel, c.row_tiles * c.lanes, kThreads, kShared, k.pair ? 2 : 1, st, k, m_cache, m_q);
+    cudaError_t e = launch_early(kernel, c.row_tiles * c.lanes, kThreads, kShared, 1, st, k, m_cache, m_q);
     if (e != cudaSuccess) return launched("sim_op_latent_decode", e);
     // Few rows: a block shares the pieces of one; many: a warp has a row of its
     // own.  2 x 128 heads 27.3 us (a warp a row 54.5), 8 x 128 30.4 (44.5), 64 x 16 60.2
@@ -744,7 +735,6 @@ extern "C" int sim_op_latent_decode(const sim_op_latent_decode_t *a, void *strea
         const uint32_t box[3] = {64, (uint32_t)k.q_pad, 1};
         if (!box_map(&mq, a->q, bf, 3, size, stride, box)) return SIM_ERR_CUDA;
     }
-    k.pair = c.row_tiles % 2 == 0 && !k.scattered;
     const cudaStream_t st = (cudaStream_t)stream;
     return bf ? run<__nv_bfloat16>(k, m, mq, c, st) : run<__half>(k, m, mq, c, st);
 }

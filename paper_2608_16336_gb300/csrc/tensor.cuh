@@ -69,14 +69,6 @@ __device__ __forceinline__ void copy_box_3d(uint32_t dst, const CUtensorMap *map
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
-// To the same place in both blocks of a pair, completing on each one's barrier.
-__device__ __forceinline__ void copy_box_2d_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1, {%2, %3}], "
-        "[%4], %5;" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(bar), "h"((uint16_t)3)
-        : "memory");
-}
 __device__ __forceinline__ void fetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // Four rows anywhere in a 2-d tensor, the map's box being one row high.
 __device__ __forceinline__ void copy_rows_4(uint32_t dst, const CUtensorMap *map, int x, int y0, int y1, int y2, int y3, uint32_t bar) {
@@ -202,12 +194,6 @@ __device__ __forceinline__ void product_commit(uint32_t bar) {
 template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-// The same arrival in both blocks of a pair.
-__device__ __forceinline__ void product_commit_pair(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                 "h"((uint16_t)3)
-                 : "memory");
-}
 // Every thread of every block of the cluster.
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
