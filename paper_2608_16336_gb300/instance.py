@@ -94,12 +94,18 @@ class Instance:
     def blocks_for(self, tokens: int) -> int:
         return -(-tokens // self.block_tokens)
 
-    def _grow(self, blocks: list[int], tokens: int) -> None:
-        need = self.blocks_for(tokens) - len(blocks)
-        if need > len(self.free):
-            raise RuntimeError("out of cache blocks: %d wanted, %d free" % (need, len(self.free)))
-        for _ in range(need):
-            blocks.append(self.free.pop())
+    def _plan(self, held, lengths):
+        """Every request's blocks with room for ``lengths`` tokens, ``held``
+        being those it has, and how many come from the end of the free list.
+        Changes nothing: an iteration that does not fit is refused here."""
+        need = [self.blocks_for(n) - len(b) for b, n in zip(held, lengths)]
+        wanted, taken, blocks = sum(need), 0, []
+        if wanted > len(self.free):
+            raise RuntimeError("out of cache blocks: %d wanted, %d free" % (wanted, len(self.free)))
+        for b, k in zip(held, need):
+            blocks.append(b + [self.free[-1 - i] for i in range(taken, taken + k)])
+            taken += k
+        return blocks, taken
 
     def release(self, request: int) -> None:
         """Takes a request out of the batch and gives its blocks back."""
@@ -113,7 +119,8 @@ class Instance:
         token of all of them.  Returns (requests, tokens, log-probabilities),
         the running ones first; the prompts are running from then on.
         ``uniform`` gives the draws (default: from PyTorch's generator), the
-        others are vectors as in ``instance_ops.sample``, one value a request."""
+        others are vectors as in ``instance_ops.sample``, one value a request.
+        A call that raises leaves the batch and the free blocks as they were."""
         s, t = self.shape, self.block_tokens
         prompts = list(prompts)
         if any(len(p) < 1 for p in prompts):
@@ -123,33 +130,23 @@ class Instance:
         decode = list(self.running)
         if not decode and not prompts:
             raise ValueError("nothing to do: no prompt and no running request")
-        for r in decode:
-            self._grow(self.running[r].blocks, self.running[r].length + 1)
-            self.running[r].length += 1
-        ids = []
-        for p in prompts:
-            blocks: list[int] = []
-            self._grow(blocks, len(p))
-            self.running[self._next] = Running(blocks, len(p), p[-1:])
-            ids.append(self._next)
-            self._next += 1
+        lengths = [self.running[r].length + 1 for r in decode] + [len(p) for p in prompts]
+        blocks, taken = self._plan([self.running[r].blocks for r in decode] + [[] for _ in prompts], lengths)
 
         # what the kernels read: positions, slots, the running requests' tables, the prompts' offsets
         nd = len(decode)
-        positions, slots = [self.running[r].length - 1 for r in decode], []
-        for r in decode:
-            q = self.running[r]
-            slots.append(q.blocks[(q.length - 1) // t] * t + (q.length - 1) % t)
-        for r in ids:
-            q = self.running[r]
-            at = np.arange(q.length)
+        positions, slots = [n - 1 for n in lengths[:nd]], []
+        for b, n in zip(blocks[:nd], lengths):
+            slots.append(b[(n - 1) // t] * t + (n - 1) % t)
+        for b, n in zip(blocks[nd:], lengths[nd:]):
+            at = np.arange(n)
             positions += at.tolist()
-            slots += (np.asarray(q.blocks)[at // t] * t + at % t).tolist()
+            slots += (np.asarray(b)[at // t] * t + at % t).tolist()
         put = lambda v, dtype: torch.tensor(v, dtype=dtype, device="cuda")
         positions, slots = put(positions, torch.int32), put(slots, torch.int64)
-        lengths = put([self.running[r].length for r in decode], torch.int32)
-        widest = max((len(self.running[r].blocks) for r in decode), default=0)
-        table = put([self.running[r].blocks + [0] * (widest - len(self.running[r].blocks)) for r in decode], torch.int32).reshape(nd, widest)
+        cached = put(lengths[:nd], torch.int32)
+        widest = max((len(b) for b in blocks[:nd]), default=0)
+        table = put([b + [0] * (widest - len(b)) for b in blocks[:nd]], torch.int32).reshape(nd, widest)
         offsets = np.cumsum([0] + [len(p) for p in prompts])
         longest = max((len(p) for p in prompts), default=0)
         starts = put(offsets.tolist(), torch.int32)
@@ -168,7 +165,7 @@ class Instance:
             if nd:  # absorbed: queries go into the latent space, values come out of it
                 inner = torch.matmul(q[:nd, :, :s.head_dim].transpose(0, 1), layer["key_up"].transpose(1, 2)).transpose(0, 1)
                 inner = torch.cat((inner, q[:nd, :, s.head_dim:]), -1)[:, None]
-                got, _ = ops.latent_decode(inner, cache, table, lengths, scale=self.scale)
+                got, _ = ops.latent_decode(inner, cache, table, cached, scale=self.scale)
                 out[:nd] = torch.matmul(got[:, 0].transpose(0, 1), layer["value_up"]).transpose(0, 1)
             if prompts:  # expanded: every head has keys and values of its own
                 keys = torch.matmul(latent[nd:], layer["key_up"]).transpose(0, 1)
@@ -182,9 +179,13 @@ class Instance:
         if uniform is None:
             uniform = torch.rand(len(logits), device="cuda")
         tokens, logprob = ops.sample(logits, uniform, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
-        for i, r in enumerate(decode + ids):
-            self.running[r].token = tokens[i:i + 1]
-        return decode + ids, tokens, logprob
+        # everything is queued: the batch changes now
+        del self.free[len(self.free) - taken:]
+        ids = decode + list(range(self._next, self._next + len(prompts)))
+        self._next += len(prompts)
+        for i, (r, b, n) in enumerate(zip(ids, blocks, lengths)):
+            self.running[r] = Running(b, n, tokens[i:i + 1])
+        return ids, tokens, logprob
 
 
 def measure(node: Instance, *, prefill_tokens=(0, 256, 1024, 4096), decodes=(0, 8, 32, 63), context: int = 512, repeats: int = 3):
