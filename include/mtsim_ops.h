@@ -124,8 +124,9 @@ int sim_op_latent_append(const sim_op_latent_append_t *args, void *cuda_stream);
  * block of zeros.  Cached rows from L on are never used, whatever they hold.
  * Scores, statistics and sums are in 32 bits; only the weights exp(s - max)
  * are rounded to the inputs' type, for their product with c (a tensor-core
- * operand; their sum is of the unrounded ones, so lse keeps 32 bits).  Types: 16-bit.  Alignment: pointers and strides of q and cache
- * are multiples of 16 bytes (8 elements), rank a multiple of 64, key_dim of 8;
+ * operand; their sum is of the unrounded ones, so lse keeps 32 bits): each by at
+ * most 2^-9 (bfloat16) or 2^-12 (float16) of itself, a float16 one below 2^-24
+ * by at most 2^-35.  Types: 16-bit.  Alignment: pointers and strides of q and cache are multiples of 16 bytes (8 elements), rank a multiple of 64, key_dim of 8;
  * cache_block is a multiple of cache_row (a cache that is one layer of several is).
  * workspace: sim_op_latent_decode_workspace() bytes for the same sizes,
  * 256-byte aligned, contents need not be set; not to be shared by calls that overlap. */

@@ -118,6 +118,7 @@ struct Piece {
 template <typename T, int TILE>
 __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_cache, const __grid_constant__ CUtensorMap m_q) {
     using Z = Shape<TILE>;
+    using R = WeightRange<T>;
     extern __shared__ __align__(1024) unsigned char smem[];
     // Q's column blocks hold only the rows there are (rounded up to 16, 32 or
     // 64): a product reads 64, and what it finds past them (the
@@ -401,14 +402,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
                     m1 = fmaxf(m1, __shfl_xor_sync(~0u, m1, o));
                 }
                 const float high0 = real0 ? m0 * a.scale_log2 : -INFINITY, high1 = real1 ? m1 * a.scale_log2 : -INFINITY;
-                // sums are rescaled only when the maximum has grown by 2^8: weights up to 256 are as exact
-                const bool grow0 = high0 > top0 + 8.f || (top0 == -INFINITY && high0 > -INFINITY);
-                const bool grow1 = high1 > top1 + 8.f || (top1 == -INFINITY && high1 > -INFINITY);
+                // sums are rescaled only when the maximum has grown by 2^grow: weights up to that are as exact
+                const bool grow0 = high0 > top0 + R::grow || (top0 == -INFINITY && high0 > -INFINITY);
+                const bool grow1 = high1 > top1 + R::grow || (top1 == -INFINITY && high1 > -INFINITY);
                 float keep0 = 1.f, keep1 = 1.f;
                 if (grow0) keep0 = top0 == -INFINITY ? 0.f : exp2_fast(top0 - high0), top0 = high0;
                 if (grow1) keep1 = top1 == -INFINITY ? 0.f : exp2_fast(top1 - high1), top1 = high1;
                 sum0 *= keep0, sum1 *= keep1;
-                const float base0 = top0 == -INFINITY ? 0.f : -top0, base1 = top1 == -INFINITY ? 0.f : -top1;
+                const float base0 = top0 == -INFINITY ? 0.f : R::raise - top0, base1 = top1 == -INFINITY ? 0.f : R::raise - top1;
                 uint32_t p[TILE / 4];
 #pragma unroll
                 for (int e = 0; e < TILE / 8; ++e) {
@@ -515,8 +516,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
             if (lane % 4 == 0) {
                 if (whole) {
                     const int64_t at = (int64_t)pc.b * a.new_tokens * a.heads;
-                    if (real0 && a.lse) a.lse[at + f0] = sum0 != 0.f ? (top0 + log2f(sum0)) * 0.6931471805599453f : -INFINITY;
-                    if (real1 && a.lse) a.lse[at + f1] = sum1 != 0.f ? (top1 + log2f(sum1)) * 0.6931471805599453f : -INFINITY;
+                    if (real0 && a.lse) a.lse[at + f0] = sum0 != 0.f ? (top0 + (log2f(sum0) - R::raise)) * 0.6931471805599453f : -INFINITY;
+                    if (real1 && a.lse) a.lse[at + f1] = sum1 != 0.f ? (top1 + (log2f(sum1) - R::raise)) * 0.6931471805599453f : -INFINITY;
                 } else {
                     a.stats[slot * kRows + r0] = make_float2(top0, sum0);
                     a.stats[slot * kRows + r0 + 8] = make_float2(top1, sum1);
@@ -604,7 +605,7 @@ template <typename T, int WARPS> __global__ void __launch_bounds__(kJoinWarps * 
             if (all != 0.f) w = make_uint2(pack2<T>(v[j].x * inv, v[j].y * inv), pack2<T>(v[j].z * inv, v[j].w * inv));
             *(uint2 *)(out + 128 * j + 4 * lane) = w;
         }
-    if (a.lse && lane == 0) a.lse[row] = all != 0.f ? (m + log2f(all)) * 0.6931471805599453f : -INFINITY;
+    if (a.lse && lane == 0) a.lse[row] = all != 0.f ? (m + (log2f(all) - WeightRange<T>::raise)) * 0.6931471805599453f : -INFINITY;
 }
 
 // How the work is cut: row tiles side by side, and parts of the line of tiles.

@@ -78,6 +78,7 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
           const __grid_constant__ CUtensorMap m_k, const __grid_constant__ CUtensorMap m_kr,
           const __grid_constant__ CUtensorMap m_v) {
     using Z = Shape<TILES>;
+    using R = WeightRange<T>;
     constexpr int kKeys = Z::keys, kSlotBytes = Z::slot_bytes, kSoftWarps = Z::soft_warps;
     constexpr int ring_offset = Z::q_slots * kQBytes;
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -322,9 +323,9 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
                 m0 = fmaxf(m0, x[c]), m1 = fmaxf(m1, x[c + 1]), m2 = fmaxf(m2, x[c + 2]), m3 = fmaxf(m3, x[c + 3]);
             }
             const float high = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;
-            // The sums are rescaled only when the maximum has grown by 2^8:
-            // until then weights up to 256 are as exact, and O stays where it is.
-            const bool grow = high > top + 8.f || (top == -INFINITY && high > -INFINITY);
+            // The sums are rescaled only when the maximum has grown by 2^grow:
+            // until then weights up to that are as exact, and O stays where it is.
+            const bool grow = high > top + R::grow || (top == -INFINITY && high > -INFINITY);
             if (__any_sync(~0u, grow)) {
                 const float keep = grow ? (top == -INFINITY ? 0.f : exp2_fast(top - high)) : 1.f;
                 if (grow) top = high;
@@ -343,7 +344,7 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
                     }
                 }
             }
-            const float base = top == -INFINITY ? 0.f : -top;
+            const float base = top == -INFINITY ? 0.f : R::raise - top;
             float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
             uint32_t p[kKeys / 2];
 #pragma unroll
@@ -425,14 +426,14 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
                             make_uint2(pack2<T>(v[j].x * inv, v[j].y * inv), pack2<T>(v[j].z * inv, v[j].w * inv));
                 }
                 if (a.lse && k8 == 0 && mine < there)
-                    a.lse[(int64_t)(q0 + base + mine) * a.heads + h] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+                    a.lse[(int64_t)(q0 + base + mine) * a.heads + h] = sum != 0.f ? (top + (log2f(sum) - R::raise)) * 0.6931471805599453f : -INFINITY;
             }
             __syncwarp();
             cluster_sync();  // the others have read
         } else {
             // a sum of 0 is a row that sees nothing: zeros; a sum that is no number stays one
             if (row < rows && a.lse)
-                a.lse[(int64_t)(q0 + row) * a.heads + h] = sum != 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+                a.lse[(int64_t)(q0 + row) * a.heads + h] = sum != 0.f ? (top + (log2f(sum) - R::raise)) * 0.6931471805599453f : -INFINITY;
             const float inv = sum != 0.f ? 1.f / sum : 0.f;
             T *out = (T *)a.out + (int64_t)(q0 + row) * a.out_row + h * a.out_head;
             if (nt > 0) {
