@@ -409,13 +409,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
                 if (grow0) keep0 = top0 == -INFINITY ? 0.f : exp2_fast(top0 - high0), top0 = high0;
                 if (grow1) keep1 = top1 == -INFINITY ? 0.f : exp2_fast(top1 - high1), top1 = high1;
                 sum0 *= keep0, sum1 *= keep1;
-                const float base0 = top0 == -INFINITY ? 0.f : R::raise - top0, base1 = top1 == -INFINITY ? 0.f : R::raise - top1;
+                float base0 = top0 == -INFINITY ? 0.f : R::raise - top0, base1 = top1 == -INFINITY ? 0.f : R::raise - top1;
+                float by = a.scale_log2;
+                if (__any_sync(~0u, (beyond_fused(top0) && top0 != -INFINITY) || (beyond_fused(top1) && top1 != -INFINITY))) {
+                    by = 1.f, base0 = base1 = R::raise;
+#pragma unroll
+                    for (int e = 0; e < TILE / 2; ++e) x[e] = below_top(x[e], a.scale_log2, e & 2 ? top1 : top0);
+                }
                 uint32_t p[TILE / 4];
 #pragma unroll
                 for (int e = 0; e < TILE / 8; ++e) {
                     float a0, a1, b0, b1;
-                    fma2(a0, a1, x[4 * e], x[4 * e + 1], a.scale_log2, a.scale_log2, base0, base0);
-                    fma2(b0, b1, x[4 * e + 2], x[4 * e + 3], a.scale_log2, a.scale_log2, base1, base1);
+                    fma2(a0, a1, x[4 * e], x[4 * e + 1], by, by, base0, base0);
+                    fma2(b0, b1, x[4 * e + 2], x[4 * e + 3], by, by, base1, base1);
                     a0 = exp2_fast(a0), a1 = exp2_fast(a1), b0 = exp2_fast(b0), b1 = exp2_fast(b1);
                     sum0 += a0 + a1, sum1 += b0 + b1;
                     p[2 * e] = pack2<T>(a0, a1), p[2 * e + 1] = pack2<T>(b0, b1);

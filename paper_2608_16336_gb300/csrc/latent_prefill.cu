@@ -53,7 +53,7 @@ struct Args {
     int groups;      // of heads that run side by side (their keys and values stay in L2)
     int row_blocks;  // of a block's queries
     int split;       // blocks that share queries
-    float scale_log2;  // |scale| log2(e)
+    float scale_log2, unscale;  // |scale| log2(e), and one over it
     bool negative;
 };
 
@@ -325,11 +325,15 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
             const float high = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * scale;
             // The sums are rescaled only when the maximum has grown by 2^grow:
             // until then weights up to that are as exact, and O stays where it is.
-            const bool grow = high > top + R::grow || (top == -INFINITY && high > -INFINITY);
-            if (__any_sync(~0u, grow)) {
-                const float keep = grow ? (top == -INFINITY ? 0.f : exp2_fast(top - high)) : 1.f;
+            const bool grow = high > top + R::grow;
+            if (__any_sync(~0u, grow || beyond_fused(top))) {
+                const float keep = grow ? exp2_fast(top - high) : 1.f;
                 if (grow) top = high;
                 sum *= keep;
+                if (beyond_fused(top)) {
+#pragma unroll
+                    for (int c = 0; c < kKeys; ++c) x[c] = below_top(x[c], scale, top) * a.unscale;  // times the scale again below
+                }
                 if (i > 0) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -344,7 +348,7 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
                     }
                 }
             }
-            const float base = top == -INFINITY ? 0.f : R::raise - top;
+            const float base = beyond_fused(top) ? R::raise : R::raise - top;
             float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
             uint32_t p[kKeys / 2];
 #pragma unroll
@@ -518,6 +522,7 @@ extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *str
     k.head_blocks = (a->head_dim + 63) / 64, k.key_blocks = (a->key_dim + 63) / 64, k.value_blocks = (a->value_dim + 63) / 64;
     k.value_dim = a->value_dim, k.causal = a->causal;
     k.scale_log2 = std::fmax(std::fabs(a->scale) * 1.4426950408889634f, 1e-30f);  // not 0: a masked score is -infinity times it
+    k.unscale = 1.f / k.scale_log2;
     k.negative = a->scale < 0;
     const int64_t longest = a->longest < a->q_rows ? a->longest : a->q_rows;
     // One tile a block where most prompts leave the second one empty and keys

@@ -46,3 +46,37 @@ def test_prefill_many_small_weights(nq, nk, heads, dtype):
     out, lse = ops.latent_prefill(q, key, shared, value, qo, ko, scale=1.0, longest=nq)
     check_prefill(q, key, shared, value, qo, ko, 1.0, out, lse)
     assert float(out.max()) > 0
+
+
+# Scores of 1e6 and more, far apart: all of the weight is on the largest.  The
+# result is its value, rounded once; a score's 32-bit sum is good to 1e-6 of the
+# products' absolute sum, which is about five times the largest score.
+def one_hot(s, value, out, lse):
+    assert torch.allclose(lse.double(), s.amax(1), rtol=1e-5)
+    alone = torch.topk(s, 2).values.diff()[:, 0].abs() > 1e-5 * s.abs().max()  # no two compete
+    assert alone.double().mean() > 0.99
+    want = value[s.argmax(1)].double()[alone]
+    assert ((out[alone].double() - want).abs() <= 2.0 ** -8 * want.abs()).all()
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("dtype,size", [(BF, 1e5), (BF, 2e3), (HF, 1e4), (HF, 1e3)])
+@pytest.mark.parametrize("n,heads", [(90, 16), (700, 16), (700, 128), (5000, 16)])
+def test_decode_very_large_scores(n, heads, dtype, size):
+    q, cache, table, lengths = decode_case([n, 40], 1, heads, 512, 64, 16, dtype, seed=n)
+    q, cache = (q.float() * size).to(dtype), (cache.float() * size).to(dtype)
+    out, lse = ops.latent_decode(q, cache, table, lengths, scale=0.1)
+    for b, m in enumerate((n, 40)):
+        rows = cache[table[b, :-(-m // 16)].long()].reshape(-1, 576)[:m]
+        one_hot(q[b, 0].double() @ rows.double().T * 0.1, rows[:, :512], out[b, 0], lse[b, 0])
+
+
+@pytest.mark.parametrize("dtype,size", [(BF, 1e5), (BF, 2e3), (HF, 1e4), (HF, 1e3)])
+@pytest.mark.parametrize("nq,nk,heads", [(100, 100, 2), (130, 3000, 1), (300, 700, 40)])
+def test_prefill_very_large_scores(nq, nk, heads, dtype, size):
+    args = prefill_case([nq], [nk], heads, 128, 64, 128, dtype, seed=nk)
+    q, key, shared, value = [(t.float() * size).to(dtype) for t in args[:4]]
+    out, lse = ops.latent_prefill(q, key, shared, value, *args[4:], scale=0.1, longest=nq, causal=False)
+    for h in range(heads):
+        s = q[:, h].double() @ torch.cat((key[:, h], shared), 1).double().T * 0.1
+        one_hot(s, value[:, h], out[:, h], lse[:, h])
