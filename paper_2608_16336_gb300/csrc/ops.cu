@@ -80,6 +80,9 @@ unsigned prefill_faults();
 }  // namespace mtop
 
 extern "C" int sim_op_faults(void) {
+    // (a copy alone would not wait for streams that do not wait for the default one)
+    const cudaError_t e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) return mtop::launched("sim_op_faults", e);
     const unsigned d = mtop::decode_faults(), p = mtop::prefill_faults(), n = d + p;
     return d == ~0u || p == ~0u || n > 0x7FFFFFFFu ? mtop::fail(SIM_ERR_CUDA, "the fault counter cannot be read") : (int)n;
 }
