@@ -13,8 +13,10 @@ from PyTorch's allocator on that stream.  Arguments are checked here (shape,
 type, place, alignment: ``ValueError`` or ``TypeError``) and again by the
 library (``mtsim.SimError``).  Values on the device are bounded by the kernels
 as the header states.  The operators are forward only: a tensor that asks for a
-gradient is refused while gradients are enabled (the gradient of ``rotary`` is
-``rotary`` with ``inverse=True``).
+gradient is refused while gradients are enabled, one with a forward-mode tangent
+while those are (the gradient of ``rotary`` is ``rotary`` with
+``inverse=True``).  What a call writes into a tensor of the caller's counts as a
+change in place: autograd refuses a backward pass that saved it before.
 """
 from __future__ import annotations
 
@@ -23,6 +25,7 @@ import math
 from struct import Struct
 
 import torch
+from torch.autograd import forward_ad
 
 from . import mtsim
 
@@ -50,6 +53,7 @@ _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 # Scratch memory of the current device on a stream, without a tensor around it: 5 us less of a small call's 16.
 _scratch = getattr(torch._C, "_cuda_cudaCachingAllocator_raw_alloc", None) or (
     lambda nbytes, stream: torch.cuda.caching_allocator_alloc(nbytes, stream=stream))
+_changed = getattr(torch._C, "_increment_version", None) or torch.autograd.graph.increment_version  # of a tuple of tensors
 _release = getattr(torch._C, "_cuda_cudaCachingAllocator_raw_delete", None) or torch.cuda.caching_allocator_delete
 
 
@@ -81,17 +85,18 @@ def faults() -> int:
     return n
 
 
-def _place(tensors, others=()) -> int:
-    """The one CUDA device, the current one, that every tensor is on; ``tensors`` may not ask for gradients."""
+def _place(*tensors) -> int:
+    """The one CUDA device, the current one, that every tensor is on; none may ask for a gradient."""
     device = tensors[0].get_device()
     for t in tensors:
         if t.get_device() != device:
             raise ValueError("every tensor must be on the same CUDA device")
         if t.requires_grad and torch.is_grad_enabled():
             raise ValueError("forward only: call under torch.no_grad() or detach the tensors")
-    for t in others:
-        if t.get_device() != device:
-            raise ValueError("every tensor must be on the same CUDA device")
+    if forward_ad._current_level >= 0 and torch._C._is_fwd_grad_enabled():
+        for t in tensors:
+            if forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("no forward-mode gradients: a tensor has a tangent")
     if device < 0:
         raise ValueError("the tensors must be on a CUDA device")
     if device != _current_device():
@@ -200,13 +205,14 @@ def rotary(x, positions, frequencies, *, layout="interleaved", offset=0, amplitu
         out = torch.empty(shape, dtype=x.dtype, device=x.device)
     xs, ys = _rows("x", x, shape), _rows("out", out, shape)
     code = _type("x", x, out)
-    device = _place((x, out), (positions, frequencies))
+    device = _place(x, out, positions, frequencies)
     rc = (_LIB or lib()).sim_op_rotary(
         ROTARY.pack(x.data_ptr(), out.data_ptr(), positions.data_ptr(), frequencies.data_ptr(), n, xs[0], xs[1], ys[0], ys[1],
                     heads, dim, rot, offset, code, _layout(layout), wide, 1 if inverse else 0, amplitude),
         _stream_of(device))
     if rc:
         _failed(rc)
+    _changed((out,))
     return out
 
 
@@ -226,7 +232,7 @@ def latent_append(latent, key, positions, frequencies, slots, cache, *, layout="
         raise TypeError("slots must be int64, not %s" % slots.dtype)
     _packed("slots", slots, (n,))
     code = _type("latent", latent, key, cache)
-    device = _place((latent, key, cache), (positions, frequencies, slots))
+    device = _place(latent, key, cache, positions, frequencies, slots)
     rc = (_LIB or lib()).sim_op_latent_append(
         APPEND.pack(latent.data_ptr(), key.data_ptr(), cache.data_ptr(), positions.data_ptr(), slots.data_ptr(),
                     frequencies.data_ptr(), n, ls[0], ks[0], cs[0], cs[1], blocks, block, rank, rot, code, _layout(layout), wide,
@@ -234,6 +240,7 @@ def latent_append(latent, key, positions, frequencies, slots, cache, *, layout="
         _stream_of(device))
     if rc:
         _failed(rc)
+    _changed((cache,))
     return cache
 
 
@@ -268,7 +275,7 @@ def latent_decode(q, cache, table, lengths, *, scale, out=None, lse=None):
         raise TypeError("lse must be float32")
     _packed("lse", lse, (b, new, heads))
     code = _type("q", q, cache, out, wide=False)
-    device = _place((q, cache, out, lse), (table, lengths))
+    device = _place(q, cache, out, lse, table, lengths)
     L = _LIB or lib()
     size = (device, b, new, heads, rank)
     nbytes = _WORKSPACE.get(size)
@@ -286,6 +293,7 @@ def latent_decode(q, cache, table, lengths, *, scale, out=None, lse=None):
         _release(work)  # what the stream allocates next comes after this call's kernels
     if rc:
         _failed(rc)
+    _changed((out, lse))
     return out, lse
 
 
@@ -323,7 +331,7 @@ def latent_prefill(q, key, shared, value, q_offsets, k_offsets, *, scale, longes
         raise TypeError("lse must be float32")
     _packed("lse", lse, (n, heads))
     code = _type("q", q, key, shared, value, out, wide=False)
-    device = _place((q, key, shared, value, out, lse), (q_offsets, k_offsets))
+    device = _place(q, key, shared, value, out, lse, q_offsets, k_offsets)
     rc = (_LIB or lib()).sim_op_latent_prefill(
         PREFILL.pack(q.data_ptr(), key.data_ptr(), shared.data_ptr(), value.data_ptr(), q_offsets.data_ptr(),
                      k_offsets.data_ptr(), out.data_ptr(), lse.data_ptr(), qs[0], qs[1], ks[0], ks[1], ss[0], vs[0], vs[1],
@@ -331,6 +339,7 @@ def latent_prefill(q, key, shared, value, q_offsets, k_offsets, *, scale, longes
         _stream_of(device))
     if rc:
         _failed(rc)
+    _changed((out, lse))
     return out, lse
 
 
@@ -352,7 +361,7 @@ def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=N
     if logprob is None:
         logprob = torch.empty(rows, dtype=torch.float32, device=logits.device)
     code = _type("logits", logits)
-    device = logits.get_device()
+    used = [logits]
 
     def vector(name, t, dtype):
         """The address of a vector of one value a row (0: none)."""
@@ -362,16 +371,16 @@ def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=N
             raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
         if t.dim() != 1 or t.shape[0] != rows or not t.is_contiguous():
             raise ValueError("%s must be a contiguous vector of %d values" % (name, rows))
-        if t.get_device() != device:
-            raise ValueError("every tensor must be on the same CUDA device")
+        used.append(t)
         return t.data_ptr()
 
     real = torch.float32
     args = SAMPLE.pack(logits.data_ptr(), vector("uniform", uniform, real), vector("temperature", temperature, real),
                        vector("top_k", top_k, torch.int32), vector("top_p", top_p, real), vector("min_p", min_p, real),
                        vector("out", out, torch.int64), vector("logprob", logprob, real), stride, rows, vocab, code)
-    _place((logits,))
+    device = _place(*used)
     rc = (_LIB or lib()).sim_op_sample(args, _stream_of(device))
     if rc:
         _failed(rc)
+    _changed((out, logprob))
     return out, logprob
