@@ -160,6 +160,9 @@ size_t sim_op_latent_decode_workspace(int32_t requests, int32_t new_tokens, int3
  * prefix), or every key with causal = 0.  Scores are
  *   s_ij = scale * (<q[i][h][0 .. head_dim), key[j][h]> + <q[i][h][head_dim ..), shared[j]>)
  * with the rotated key `shared` common to all heads; out and lse as above.
+ * Keys and values that a query does not see have no part in its result, whatever
+ * they hold (a call with infinities or NaN in tokens that some queries see and
+ * others not takes up to twice the time).
  * Offsets must not decrease; they are bounded by q_rows and k_rows, and at
  * most `longest` queries of a request are computed (`longest` also decides,
  * with the numbers of rows, requests and heads, how the work is cut, and so the last bits).  Rows that belong to no

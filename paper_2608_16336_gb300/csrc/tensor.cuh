@@ -15,6 +15,7 @@ __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }
+__device__ __forceinline__ void bar_retire(uint32_t bar) { asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void bar_init_done() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -225,6 +226,28 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+
+// Pairs of 16-bit numbers.  spoil() adds 0 times a pair: 0 stays 0 unless a
+// number is infinite or NaN.  finite_only() puts zeros in the place of such.
+template <typename T> struct Pair;
+template <> struct Pair<__nv_bfloat16> {
+    typedef __nv_bfloat162 two;
+    static constexpr uint32_t exponent = 0x7F80;
+};
+template <> struct Pair<__half> {
+    typedef __half2 two;
+    static constexpr uint32_t exponent = 0x7C00;
+};
+template <typename T> __device__ __forceinline__ void spoil(uint32_t &sum, uint32_t w) {
+    typedef typename Pair<T>::two two;
+    const uint32_t zero = 0;
+    *(two *)&sum = __hfma2(*(const two *)&w, *(const two *)&zero, *(two *)&sum);
+}
+__device__ __forceinline__ bool spoiled(uint32_t sum) { return sum & 0x7FFF7FFF; }
+template <typename T> __device__ __forceinline__ uint32_t finite_only(uint32_t w) {
+    constexpr uint32_t e = Pair<T>::exponent;
+    return w & ((w & e) == e ? 0xFFFF0000u : ~0u) & ((w >> 16 & e) == e ? 0xFFFFu : ~0u);
 }
 
 // How softmax weights are held as an operand of the product with the values.
