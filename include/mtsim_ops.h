@@ -121,7 +121,8 @@ int sim_op_latent_append(const sim_op_latent_append_t *args, void *cuda_stream);
  * A row that sees nothing gives zeros and lse = -infinity; one whose scores
  * are NaN or +infinity gives NaN.  lengths are taken
  * as at most table_blocks * T; a table entry outside [0, blocks) stands for a
- * block of zeros.  Cached rows from L on are never used, whatever they hold.
+ * block of zeros.  Cached rows from L on are never used, whatever they hold,
+ * and a new token's result has no part of those after it.
  * Scores, statistics and sums are in 32 bits; only the weights exp(s - max)
  * are rounded to the inputs' type, for their product with c (a tensor-core
  * operand; their sum is of the unrounded ones, so lse keeps 32 bits): each by at

@@ -47,14 +47,14 @@ template <int TILE> struct Shape {
 };
 
 struct Args {
-    const void *q;
+    const void *q, *cache;
     const int32_t *table, *lengths;
     void *out;
     float *lse;
     int *first;      // [requests + 1]: the line's first tile of each request
     float *sums;     // [parts][2][64][rank]: the unfinished O of a part's first and last piece
     float2 *stats;   // [parts][2][64]: maximum and sum of weights
-    int64_t q_request, q_token, q_head, out_request, out_token, out_head, table_row;
+    int64_t q_request, q_token, q_head, out_request, out_token, out_head, cache_row, table_row;
     int64_t blocks, most;  // most: tokens a table can name
     int requests, new_tokens, heads, rank, width;
     int block_tokens, row_ratio;  // cache_block / cache_row
@@ -75,6 +75,7 @@ template <int TILE> struct Barriers {
     uint64_t p_ready[Shape<TILE>::weights], pv_done[Shape<TILE>::weights], o_free;
     uint32_t tmem;
     int first_request, first_tile, total;
+    int spoiled[2];  // the last even and odd piece whose cached rows had infinities or NaN taken out
 };
 
 __device__ __forceinline__ int tokens_of(const Args &a, int b) {
@@ -115,7 +116,44 @@ struct Piece {
     }
 };
 
-template <typename T, int TILE>
+// Cached rows [from, to) of a tile that not all new tokens see.  A weight of
+// 0 times infinity or NaN is not 0, so these become zeros (a thread takes 16 bytes of every second row),
+template <typename T> __device__ __noinline__ void clean_rows(unsigned char *at, int from, int to) {
+    for (int r = from + threadIdx.x / 64; r < to; r += 2) {
+        uint4 &w = *(uint4 *)(at + r * 128);
+        w = make_uint4(finite_only<T>(w.x), finite_only<T>(w.y), finite_only<T>(w.z), finite_only<T>(w.w));
+    }
+}
+// and are added at the end to what the sums of the rows that see them have:
+// tokens [j, past) of request b, of which this thread's two rows see those below see0 and see1.
+template <typename T> __device__ __noinline__ void add_cleaned(const Args &a, int b, int j, int past, int see0, int see1, uint32_t o_at) {
+    const int lane = threadIdx.x % 32;
+    const int32_t *table = a.table + b * a.table_row;
+    for (; j < past; ++j) {
+        const int blk = j / a.block_tokens, id = table[blk];
+        if (id < 0 || id >= a.blocks) continue;
+        const T *row = (const T *)a.cache + ((int64_t)id * a.row_ratio + (j - blk * a.block_tokens)) * a.cache_row + 2 * (lane % 4);
+        for (int c = 0; c < a.rank / 64; ++c, row += 64) {
+            uint32_t o[32];
+            tmem_ld_rows<64>(o_at + 64 * c, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float x = elem<T>::to(row[e / 2 * 8 + e % 2]);
+                uint32_t &o0 = o[e / 2 * 4 + e % 2], &o1 = o[e / 2 * 4 + 2 + e % 2];
+                if (!(fabsf(x) < INFINITY) && j < see0) o0 = __float_as_uint(__uint_as_float(o0) + x);
+                if (!(fabsf(x) < INFINITY) && j < see1) o1 = __float_as_uint(__uint_as_float(o1) + x);
+            }
+            __syncwarp();
+            tmem_st_rows64(o_at + 64 * c, o);
+            tmem_wait_st();
+        }
+    }
+}
+
+// SEVERAL: calls of more than one new token (3 requests of 90,001 to 130,000 tokens, two
+// new ones 92.0 us; without the two steps above 89.6, which calls of one do not pay).
+template <typename T, int TILE, bool SEVERAL>
 __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_cache, const __grid_constant__ CUtensorMap m_q) {
     using Z = Shape<TILE>;
     using R = WeightRange<T>;
@@ -147,6 +185,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
             bar_init(smem_addr(&bars->pv_done[s]), 1);
         }
         bar_init(smem_addr(&bars->o_free), kSoftWarps * 32);
+        bars->spoiled[0] = bars->spoiled[1] = -1;
         bar_init_done();
     }
     if (warp == kSoftWarps) tmem_alloc(smem_addr(&bars->tmem), kCols);
@@ -380,6 +419,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
                         for (int e = from * 8 + threadIdx.x; e < TILE * 8; e += kSoftWarps * 32)
                             *(uint4 *)(stage + c * Z::block_bytes + e * 16) = make_uint4(0, 0, 0, 0);
                 }
+                if (SEVERAL && (t + 1) * TILE > fewest) {
+                    // (little code: it runs once a request, and fetching it is what it costs)
+                    bar_test(smem_addr(&bars->full[stage_of]), (i / a.stages) & 1);  // has completed: what the copy wrote is visible
+                    const int c = threadIdx.x / 8 % 8, from = max(fewest - t * TILE, 0), to = c < value_blocks ? min(tokens - t * TILE, TILE) : 0;
+                    unsigned char *at = smem + stage_offset + stage_of * stage_bytes + c * Z::block_bytes + threadIdx.x % 8 * 16;
+                    uint32_t sum = 0;
+#pragma unroll 1
+                    for (int r = from + threadIdx.x / 64; r < to; r += 2) {
+                        const uint4 w = *(const uint4 *)(at + r * 128);
+                        spoil<T>(sum, w.x), spoil<T>(sum, w.y), spoil<T>(sum, w.z), spoil<T>(sum, w.w);
+                    }
+                    if (spoiled(sum)) clean_rows<T>(at, from, to), bars->spoiled[k & 1] = k;
+                    __syncwarp();
+                }
                 if ((t + 1) * TILE > fewest) {
                     const int c0 = t * TILE + 2 * (lane % 4);
 #pragma unroll
@@ -411,7 +464,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
                 sum0 *= keep0, sum1 *= keep1;
                 float base0 = top0 == -INFINITY ? 0.f : R::raise - top0, base1 = top1 == -INFINITY ? 0.f : R::raise - top1;
                 float by = a.scale_log2;
-                if (__any_sync(~0u, (beyond_fused(top0) && top0 != -INFINITY) || (beyond_fused(top1) && top1 != -INFINITY))) {
+                // (a row that is infinite or NaN leaves its neighbours' rounding as it is)
+                if (__any_sync(~0u, (beyond_fused(top0) && fabsf(top0) < INFINITY) || (beyond_fused(top1) && fabsf(top1) < INFINITY))) {
                     by = 1.f, base0 = base1 = R::raise;
 #pragma unroll
                     for (int e = 0; e < TILE / 2; ++e) x[e] = below_top(x[e], a.scale_log2, e & 2 ? top1 : top0);
@@ -471,6 +525,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_decode(const __grid_constant__ 
             const float inv0 = sum0 != 0.f ? 1.f / sum0 : 0.f, inv1 = sum1 != 0.f ? 1.f / sum1 : 0.f;
             float *sums = a.sums + (slot * kRows + warp * 16) * a.rank;
             T *out = (T *)a.out + pc.b * a.out_request;
+            if (SEVERAL && pc.t1 * TILE > fewest) {
+                asm volatile("bar.sync 1, %0;" ::"n"(kSoftWarps * 32) : "memory");  // all have said whether there were some
+                if (*(volatile int *)&bars->spoiled[k & 1] == k) add_cleaned<T>(a, pc.b, max(fewest, pc.t0 * TILE), min(tokens, pc.t1 * TILE), see0, see1, o_at);
+            }
             // Fragments hold 8 bytes of a row; through the (now idle) rows of P
             // they leave as 128 bytes of a row.  A warp has 16 rows of its own there.
             for (int c = 0; c < value_blocks; ++c) {
@@ -634,9 +692,10 @@ Cut cut_for(int sms, int64_t requests, int64_t new_tokens, int64_t heads, int64_
 }
 
 template <typename T> int run(const Args &k, const CUtensorMap &m_cache, const CUtensorMap &m_q, const Cut &c, cudaStream_t st) {
-    auto kernel = k.tile == 32 ? k_decode<T, 32> : k_decode<T, 64>;
-    static std::atomic<uint64_t> told[2];
-    if (!allow_shared((const void *)kernel, kShared, told[k.tile == 32])) return SIM_ERR_CUDA;
+    const bool several = k.new_tokens > 1;
+    auto kernel = k.tile == 32 ? (several ? k_decode<T, 32, true> : k_decode<T, 32, false>) : several ? k_decode<T, 64, true> : k_decode<T, 64, false>;
+    static std::atomic<uint64_t> told[4];
+    if (!allow_shared((const void *)kernel, kShared, told[2 * (k.tile == 32) + several])) return SIM_ERR_CUDA;
     cudaError_t e = launch_early(kernel, c.row_tiles * c.lanes, kThreads, kShared, 1, st, k, m_cache, m_q);
     if (e != cudaSuccess) return launched("sim_op_latent_decode", e);
     // Few rows: a block shares the pieces of one; many: a warp has a row of its
@@ -701,12 +760,12 @@ extern "C" int sim_op_latent_decode(const sim_op_latent_decode_t *a, void *strea
     const Cut c = cut_for(sms, a->requests, a->new_tokens, a->heads, a->rank);
     if (a->workspace_bytes < c.bytes()) return fail(SIM_ERR_ARG, "the workspace must have %zu bytes", c.bytes());
     Args k;
-    k.q = a->q, k.table = a->table, k.lengths = a->lengths, k.out = a->out, k.lse = a->lse;
+    k.q = a->q, k.cache = a->cache, k.table = a->table, k.lengths = a->lengths, k.out = a->out, k.lse = a->lse;
     k.first = (int *)a->workspace;
     k.sums = (float *)((char *)a->workspace + c.first_bytes);
     k.stats = (float2 *)((char *)k.sums + c.sums_bytes);
     k.q_request = a->q_request, k.q_token = a->q_token, k.q_head = a->q_head;
-    k.out_request = a->out_request, k.out_token = a->out_token, k.out_head = a->out_head, k.table_row = a->table_row;
+    k.out_request = a->out_request, k.out_token = a->out_token, k.out_head = a->out_head, k.cache_row = a->cache_row, k.table_row = a->table_row;
     k.blocks = a->blocks, k.most = most;
     k.requests = a->requests, k.new_tokens = a->new_tokens, k.heads = a->heads, k.rank = a->rank, k.width = a->rank + a->key_dim;
     k.block_tokens = a->block_tokens, k.row_ratio = (int)ratio;

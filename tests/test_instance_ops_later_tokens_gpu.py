@@ -5,7 +5,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 from paper_2608_16336_gb300 import instance_ops as ops  # noqa: E402
-from test_instance_ops_gpu import BF, HF, device, prefill_case  # noqa: E402, F401
+from test_instance_ops_gpu import BF, HF, decode_case, device, prefill_case  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 JUNK = [float("nan"), float("inf"), float("-inf")]
@@ -44,3 +44,29 @@ def test_prefill_later_values_do_not_count(nq, nk, heads, value_dim, dtype):
     assert torch.equal(torch.nan_to_num(out[at[:, 0], at[:, 1], at[:, 2]].float(), nan=0.5), torch.nan_to_num(expect, nan=0.5))
     again, _ = ops.latent_prefill(q, key, shared, junk, qo, ko, scale=0.1, longest=max(nq))
     assert torch.equal(torch.nan_to_num(again), torch.nan_to_num(out))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("lengths,new,heads,rank,block", [
+    ([64, 65, 66, 130], 4, 16, 512, 16), ([1, 2, 3, 0, 5], 5, 3, 512, 16), ([700, 64], 2, 64, 256, 24), ([90, 33], 3, 40, 128, 7),
+    ([3000], 3, 16, 512, 16), ([4100, 2500], 7, 10, 192, 33), ([300, 128], 2, 128, 512, 64)])
+def test_decode_later_rows_do_not_count(lengths, new, heads, rank, block, dtype):
+    """Each of the last new - 1 cached rows in turn holds something that is no number: the new tokens before it are untouched."""
+    q, cache, table, n = decode_case(lengths, new, heads, rank, 64, block, dtype, seed=rank + heads)
+    q = torch.where(q == 0, torch.ones_like(q), q)
+    want, lse = ops.latent_decode(q, cache, table, n, scale=0.05, out=torch.empty(len(lengths), new, heads, rank, device="cuda", dtype=dtype))
+    for back in range(new - 1):
+        junk = cache.clone()
+        for b, m in enumerate(lengths):
+            j = m - 1 - back
+            if j >= 0:
+                for e in (5 + b, 70, rank - 1):
+                    junk[int(table[b, j // block]), j % block, e] = JUNK[(b + e) % 3]
+        out, lse2 = ops.latent_decode(q, junk, table, n, scale=0.05, out=torch.empty_like(want))
+        before = new - 1 - back  # new tokens that come before the bad row
+        assert torch.equal(out[:, :before], want[:, :before]) and torch.equal(lse2[:, :before], lse[:, :before])
+        for b, m in enumerate(lengths):
+            if m - 1 - back >= 0:
+                assert not torch.isfinite(out[b, before:, :, [5 + b, 70, rank - 1]]).any()
+            else:
+                assert torch.equal(out[b], want[b]) and torch.equal(lse2[b], lse[b])
