@@ -111,12 +111,22 @@ class Instance:
         """Takes a request out of the batch and gives its blocks back."""
         self.free += self.running.pop(request).blocks[::-1]
 
+    def rewind(self, request: int, tokens: int) -> None:
+        """Takes a running request back to its first ``tokens`` cached tokens."""
+        q = self.running[request]
+        if not 1 <= tokens <= q.length:
+            raise ValueError("a request of %d tokens cannot go back to %d" % (q.length, tokens))
+        q.length = tokens
+        while len(q.blocks) > self.blocks_for(tokens):
+            self.free.append(q.blocks.pop())
+
     # -- an iteration
     @torch.no_grad()
-    def iterate(self, prompts=(), *, uniform: torch.Tensor | None = None, temperature=None, top_k=None, top_p=None, min_p=None):
+    def iterate(self, prompts=(), *, uniform: torch.Tensor | None = None, temperature=None, top_k=None, top_p=None, min_p=None,
+                advance: bool = True):
         """One iteration: prefills ``prompts`` (int64 token vectors on the device),
-        advances every running request by its last token, and draws the next
-        token of all of them.  Returns (requests, tokens, log-probabilities),
+        advances every running request by its last token (``advance=False``:
+        none), and draws the next token of all of them.  Returns (requests, tokens, log-probabilities),
         the running ones first; the prompts are running from then on.
         ``uniform`` gives the draws (default: from PyTorch's generator), the
         others are vectors as in ``instance_ops.sample``, one value a request.
@@ -127,7 +137,7 @@ class Instance:
             raise ValueError("a prompt has at least one token")
         if len(self.running) + len(prompts) > self.max_batch:
             raise ValueError("more than max_batch = %d requests" % self.max_batch)
-        decode = list(self.running)
+        decode = list(self.running) if advance else []
         if not decode and not prompts:
             raise ValueError("nothing to do: no prompt and no running request")
         lengths = [self.running[r].length + 1 for r in decode] + [len(p) for p in prompts]
@@ -190,40 +200,51 @@ class Instance:
 
 def measure(node: Instance, *, prefill_tokens=(0, 256, 1024, 4096), decodes=(0, 8, 32, 63), context: int = 512, repeats: int = 3):
     """Times iterations of ``node``: for every pair of prefill tokens (one
-    prompt) and decode requests (each with ``context`` cached tokens), the
-    median of ``repeats`` iterations in microseconds, from CUDA events, host
+    prompt) and decode requests (each with ``context`` cached tokens before the
+    iteration), the median of ``repeats`` iterations in microseconds, from CUDA events, host
     work included.  Returns [(prefill tokens, decode requests, microseconds)];
-    pairs that do not fit the instance are left out."""
+    pairs that do not fit the instance are left out.  The instance has no
+    running requests afterwards, also where an iteration raises."""
     if node.running:
         raise ValueError("the instance has running requests")
+    if context < 1 or repeats < 1:
+        raise ValueError("context and repeats must be at least 1")
     g = torch.Generator(device="cuda").manual_seed(1)
     prompt = lambda n: torch.randint(0, node.shape.vocab, (n,), generator=g, device="cuda")
-    samples = []
-    for d in decodes:
-        need = d * node.blocks_for(context + (repeats + 1) * (len(prefill_tokens) + 1) + 1)
-        if d > node.max_batch or need > len(node.free):
-            continue
-        if d:
-            for _ in range(d):  # one at a time: a prefill of all would need them expanded at once
-                node.iterate([prompt(context)])
-        for p in prefill_tokens:
-            if not p and not d or d + (p > 0) > node.max_batch or node.blocks_for(p) + d > len(node.free):
+    fits = lambda p, d: d + (p > 0) <= node.max_batch and d * node.blocks_for(context + 1) + node.blocks_for(p) <= blocks
+    blocks, samples, faults = len(node.free), [], ops.faults()
+    try:
+        for d in decodes:
+            if not any(fits(p, d) for p in prefill_tokens if p or d):
                 continue
-            times = []
-            for _ in range(repeats + 1):  # the first warms up
-                new = [prompt(p)] if p else []
-                a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-                torch.cuda.synchronize()
-                a.record()
-                ids, _, _ = node.iterate(new)
-                b.record()
-                b.synchronize()
-                times.append(a.elapsed_time(b) * 1e3)
-                if p:
-                    node.release(ids[-1])
-            samples.append((p, d, float(np.median(times[1:]))))
+            for _ in range(d):  # one at a time: a prefill of all would need them expanded at once
+                node.iterate([prompt(context)], advance=False)
+            held = list(node.running)
+            for p in prefill_tokens:
+                if not (p or d) or not fits(p, d):
+                    continue
+                times = []
+                for _ in range(repeats + 1):  # the first warms up
+                    new = [prompt(p)] if p else []
+                    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+                    torch.cuda.synchronize()
+                    a.record()
+                    ids, _, _ = node.iterate(new)
+                    b.record()
+                    b.synchronize()
+                    times.append(a.elapsed_time(b) * 1e3)
+                    for r in held:
+                        node.rewind(r, context)
+                    if p:
+                        node.release(ids[-1])
+                samples.append((p, d, float(np.median(times[1:]))))
+            for r in held:
+                node.release(r)
+    finally:
         for r in list(node.running):
             node.release(r)
+    if ops.faults() != faults:
+        raise RuntimeError("a wait inside a kernel ran out: the times are not to be used")
     return samples
 
 
