@@ -14,8 +14,8 @@ times iterations of mixed batches, ``fit_iteration_times`` gives base, a and b, 
     w = workloads.config(1, replicas=range(8), requests=500)
     node = instance.Instance(instance.Shape(layers=24), blocks=w.blocks_per_instance,
                              block_tokens=w.tokens_per_block, max_batch=w.max_batch)
-    times = instance.fit_iteration_times(instance.measure(node))
-    sim = mtsim.Simulator(instance.with_times(w, times))
+    times = instance.fit_iteration_times(instance.measure(node), per_us=10)
+    sim = mtsim.Simulator(instance.with_times(w, times, per_us=10))  # in tenths of a microsecond
 
 Weights are random; the layers are attention layers with their projections
 (plain matrix products), and ``feed_forward`` adds what else a layer does.
@@ -25,6 +25,7 @@ from __future__ import annotations
 import dataclasses
 import itertools
 import math
+import warnings
 
 import numpy as np
 import torch
@@ -248,26 +249,61 @@ def measure(node: Instance, *, prefill_tokens=(0, 256, 1024, 4096), decodes=(0, 
     return samples
 
 
-def fit_iteration_times(samples):
+def fit_iteration_times(samples, *, per_us: int = 1):
     """The integer constants (base, a, b) of base + a * prefill tokens + b *
-    decode requests microseconds nearest to the samples (least squares of
-    relative errors, none below zero)."""
+    decode requests nearest to the samples (least squares of relative errors,
+    none below zero), in units of 1 / ``per_us`` microseconds: the simulator's
+    times are whole numbers, and a token often costs less than a microsecond.
+    Warns where whole units move the time of a sample by more than 5 %;
+    ``with_times`` takes the same ``per_us``."""
+    if per_us < 1 or int(per_us) != per_us:
+        raise ValueError("per_us must be a whole number of units, at least 1")
     m = np.array([[1.0, p, d] for p, d, _ in samples])
-    t = np.array([x for _, _, x in samples], dtype=np.float64)
+    t = np.array([x for _, _, x in samples], dtype=np.float64) * per_us
     if len(t) < 3 or not (t > 0).all():
         raise ValueError("three samples or more with times above zero are needed")
-    best, found = math.inf, None
+
+    rows, best, real = m / t[:, None], math.inf, None
+    off = lambda x: float(((rows @ x - 1) ** 2).sum())
     for keep in itertools.chain.from_iterable(itertools.combinations(range(3), k) for k in (3, 2, 1)):
         x = np.zeros(3)
-        x[list(keep)] = np.linalg.lstsq(m[:, keep] / t[:, None], np.ones_like(t), rcond=None)[0]
-        off = float((((m @ x) / t - 1) ** 2).sum())
-        if (x >= 0).all() and off < best - 1e-12:
-            best, found = off, x
-    base, a, b = (int(round(v)) for v in found)
-    return max(1, base), a, b
+        x[list(keep)] = np.linalg.lstsq(rows[:, keep], np.ones_like(t), rcond=None)[0]
+        if (x >= 0).all() and off(x) < best - 1e-12:
+            best, real = off(x), x
+    # whole numbers: the pairs (a, b) around, each with its own best base
+    best, found = math.inf, None
+    around = lambda v: range(max(0, math.floor(v) - 3), math.floor(v) + 5)
+    for a, b in itertools.product(around(real[1]), around(real[2])):
+        rest = 1 - rows[:, 1] * a - rows[:, 2] * b
+        x = np.array([max(1.0, np.rint(rows[:, 0] @ rest / (rows[:, 0] @ rows[:, 0]))), a, b])
+        if off(x) < best:
+            best, found = off(x), x
+    moved = float((np.abs(m @ found - m @ real) / t).max())
+    if moved > 0.05:
+        warnings.warn("whole %s move a sample's time by %.0f %%; a larger per_us holds what was measured"
+                      % ("microseconds" if per_us == 1 else "units of 1/%d us" % per_us, 100 * moved), RuntimeWarning, stacklevel=2)
+    return tuple(int(v) for v in found)
 
 
-def with_times(w, times):
-    """A copy of workload ``w`` whose iterations take the given (base, a, b)."""
-    return dataclasses.replace(w, iter_base_us=int(times[0]), iter_us_per_prefill_token=int(times[1]),
-                               iter_us_per_decode_seq=int(times[2]))
+def with_times(w, times, *, per_us: int = 1):
+    """A copy of workload ``w`` whose iterations take the given (base, a, b),
+    constants in units of 1 / ``per_us`` microseconds as
+    ``fit_iteration_times`` gives them.  All of the copy's times are in that
+    unit then (arrivals, the migration interval and drain times are
+    multiplied), and so are the times that its simulation reports."""
+    times = dict(iter_base_us=int(times[0]), iter_us_per_prefill_token=int(times[1]), iter_us_per_decode_seq=int(times[2]))
+    if per_us < 1 or int(per_us) != per_us:
+        raise ValueError("per_us must be a whole number of units, at least 1")
+    if per_us == 1:
+        return dataclasses.replace(w, **times)
+    never = 0xFFFFFFFF
+
+    def scaled(v):
+        v = np.asarray(v)
+        x = np.where(v == never, never, v.astype(np.uint64) * np.uint64(per_us))
+        if ((x >= never) & (v != never)).any():
+            raise ValueError("times in units of 1/%d us pass 32 bits" % per_us)
+        return x.astype(v.dtype)
+
+    return dataclasses.replace(w, **times, migrate_interval_us=w.migrate_interval_us * per_us, arrival_us=scaled(w.arrival_us),
+                               drain_start_us=None if w.drain_start_us is None else scaled(w.drain_start_us))
