@@ -25,7 +25,8 @@
  *  - Return value: SIM_OK (0), SIM_ERR_ARG or SIM_ERR_CUDA (mtsim.h);
  *    sim_op_last_error() then describes the failure.  Nothing is queued when
  *    SIM_ERR_ARG is returned.
- *  - Strides are in elements.  A tensor's last dimension is contiguous.
+ *  - Strides are in elements.  A tensor's last dimension is contiguous.  The
+ *    stride of a dimension of one element is not used; inputs may have strides of 0.
  *  - Values on the device (lengths, tables, slots, offsets) cannot be checked
  *    on the host: each kernel bounds them as stated, so that no value reaches
  *    memory outside the tensors.

@@ -741,14 +741,16 @@ extern "C" int sim_op_latent_decode(const sim_op_latent_decode_t *a, void *strea
     if (rows > INT32_MAX) return fail(SIM_ERR_ARG, "requests * new_tokens * heads must be below 2^31");
     if (!a->q || !a->out || !a->lengths || (!a->table && a->table_blocks) || (!a->cache && a->blocks))
         return fail(SIM_ERR_ARG, "q, cache, table, lengths and out must not be NULL");
-    if (!aligned16(a->q) || !aligned16(a->cache) || !aligned16(a->out) || a->q_request % 8 || a->q_token % 8 || a->q_head % 8 ||
-        a->cache_block % 8 || a->cache_row % 8 || a->out_request % 8 || a->out_token % 8 || a->out_head % 8)
+    if (!aligned16(a->q) || !aligned16(a->cache) || !aligned16(a->out) || !even_stride(a->requests, a->q_request) ||
+        !even_stride(a->new_tokens, a->q_token) || !even_stride(a->heads, a->q_head) || !even_stride(a->blocks, a->cache_block) ||
+        !even_stride(a->block_tokens, a->cache_row) || !even_stride(a->requests, a->out_request) ||
+        !even_stride(a->new_tokens, a->out_token) || !even_stride(a->heads, a->out_head))
         return fail(SIM_ERR_ARG, "q, cache and out must be aligned to 16 bytes, with strides that are multiples of 8 elements");
-    // the cache is one line of rows to the copies: a block must begin on one
-    if (a->cache_row < a->rank + a->key_dim ||
-        (a->blocks > 1 && (a->cache_block < 0 || a->cache_block % a->cache_row)))
+    // the cache is one line of rows to the copies: a block must begin on one (blocks of one row are the rows)
+    const int64_t cache_row = a->block_tokens > 1 ? a->cache_row : a->blocks > 1 && a->cache_block ? a->cache_block : a->rank + a->key_dim;
+    if (cache_row < a->rank + a->key_dim || (a->blocks > 1 && (a->cache_block < 0 || a->cache_block % cache_row)))
         return fail(SIM_ERR_ARG, "cache_block must be a multiple of cache_row, which must hold a row");
-    const int64_t ratio = a->blocks > 1 ? a->cache_block / a->cache_row : a->block_tokens, cache_rows = a->blocks ? (a->blocks - 1) * ratio + a->block_tokens : 0;
+    const int64_t ratio = a->blocks > 1 ? a->cache_block / cache_row : a->block_tokens, cache_rows = a->blocks ? (a->blocks - 1) * ratio + a->block_tokens : 0;
     if (cache_rows > INT32_MAX - 1 || ratio > INT32_MAX) return fail(SIM_ERR_ARG, "the cache must span fewer than 2^31 - 1 rows");
     const int64_t most = (int64_t)a->table_blocks * a->block_tokens;
     if (most > INT32_MAX - 65536) return fail(SIM_ERR_ARG, "table_blocks * block_tokens must be below 2^31 - 2^16");
@@ -765,7 +767,7 @@ extern "C" int sim_op_latent_decode(const sim_op_latent_decode_t *a, void *strea
     k.sums = (float *)((char *)a->workspace + c.first_bytes);
     k.stats = (float2 *)((char *)k.sums + c.sums_bytes);
     k.q_request = a->q_request, k.q_token = a->q_token, k.q_head = a->q_head;
-    k.out_request = a->out_request, k.out_token = a->out_token, k.out_head = a->out_head, k.cache_row = a->cache_row, k.table_row = a->table_row;
+    k.out_request = a->out_request, k.out_token = a->out_token, k.out_head = a->out_head, k.cache_row = cache_row, k.table_row = a->table_row;
     k.blocks = a->blocks, k.most = most;
     k.requests = a->requests, k.new_tokens = a->new_tokens, k.heads = a->heads, k.rank = a->rank, k.width = a->rank + a->key_dim;
     k.block_tokens = a->block_tokens, k.row_ratio = (int)ratio;
@@ -775,7 +777,7 @@ extern "C" int sim_op_latent_decode(const sim_op_latent_decode_t *a, void *strea
     const bool bf = a->type == SIM_OP_BF16;
     CUtensorMap m, mq;
     const uint64_t size[2] = {(uint64_t)k.width, (uint64_t)k.none};
-    const int64_t stride[1] = {a->blocks ? a->cache_row : k.width};
+    const int64_t stride[1] = {a->blocks ? cache_row : k.width};
     const int64_t most_rows = (int64_t)a->new_tokens * a->heads;
     k.q_pad = most_rows <= 16 ? 16 : most_rows <= 32 ? 32 : kRows;
     const int col_blocks = (k.width + 63) / 64;

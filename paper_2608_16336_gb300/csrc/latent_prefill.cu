@@ -603,9 +603,11 @@ extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *str
         return fail(SIM_ERR_ARG, "rows must be below 2^31 - 2^16, heads and requests at most 65535");
     if (!a->q || !a->out || !a->q_offsets || !a->k_offsets || (a->k_rows && (!a->key || !a->value || (a->key_dim && !a->shared))))
         return fail(SIM_ERR_ARG, "q, key, shared, value, the offsets and out must not be NULL");
-    if (!aligned16(a->q) || !aligned16(a->key) || (a->key_dim && (!aligned16(a->shared) || a->shared_row % 8)) ||
-        !aligned16(a->value) || !aligned16(a->out) || a->q_row % 8 || a->q_head % 8 || a->key_row % 8 || a->key_head % 8 ||
-        a->value_row % 8 || a->value_head % 8 || a->out_row % 8 || a->out_head % 8)
+    const int64_t heads = a->heads;
+    if (!aligned16(a->q) || !aligned16(a->key) || (a->key_dim && (!aligned16(a->shared) || !even_stride(a->k_rows, a->shared_row))) ||
+        !aligned16(a->value) || !aligned16(a->out) || !even_stride(a->q_rows, a->q_row) || !even_stride(heads, a->q_head) ||
+        !even_stride(a->k_rows, a->key_row) || !even_stride(heads, a->key_head) || !even_stride(a->k_rows, a->value_row) ||
+        !even_stride(heads, a->value_head) || !even_stride(a->q_rows, a->out_row) || !even_stride(heads, a->out_head))
         return fail(SIM_ERR_ARG, "tensors must be aligned to 16 bytes, with strides that are multiples of 8 elements");
     const bool bf = a->type == SIM_OP_BF16;
     Args k;

@@ -47,6 +47,8 @@ inline cudaError_t launch_early(void (*kernel)(P...), unsigned grid, int threads
 int sm_count();
 
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+// Whether the stride of a dimension is made of whole vectors of 16-bit elements; one of a single element says nothing.
+inline bool even_stride(int64_t size, int64_t stride) { return size <= 1 || stride % 8 == 0; }
 
 template <typename T> struct elem;
 template <> struct elem<float> {
