@@ -280,7 +280,10 @@ def latent_decode(q, cache, table, lengths, *, scale, out=None, lse=None):
     size = (device, b, new, heads, rank)
     nbytes = _WORKSPACE.get(size)
     if nbytes is None:
-        nbytes = _WORKSPACE[size] = L.sim_op_latent_decode_workspace(b, new, heads, rank)
+        nbytes = L.sim_op_latent_decode_workspace(b, new, heads, rank)
+        if not nbytes:  # the device could not be asked: not an answer to keep
+            _failed(mtsim.SIM_ERR_CUDA)
+        _WORKSPACE[size] = nbytes
     stream = _stream_of(device)
     work = _scratch(nbytes, stream)
     try:
