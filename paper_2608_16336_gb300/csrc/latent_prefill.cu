@@ -19,7 +19,7 @@ namespace {
 // exponentials overlap the other's products.  K and V pass through a ring of
 // 16 KB slots (128 rows of 64 elements) filled by bulk copies.  Bound by the
 // tensor core and the thread that feeds it: a prompt of 8,192 tokens, 64 heads
-// takes 820 to 880 us, 1.56 to 1.68 PFLOP/s.
+// takes 865 to 905 us from GPU to GPU, 1.52 to 1.59 PFLOP/s.
 constexpr int kRows = 128;              // of a tile of queries
 constexpr int kQBytes = kRows * 128;    // of one column block (64 elements)
 constexpr int kSlots = 8;
@@ -110,10 +110,9 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
     let_next_start();
     after_previous();
     // Which rows: a group of heads after another, in a group the last (longest)
-    // row blocks of all requests first: 6 x 2,534 queries, 3 heads 35.8 us (a request
-    // after another 42.8).  With one tile, where many row blocks are empty and the
-    // blocks short (a division more shows), a request after another: 37 ragged
-    // prompts up to 300 23.2 us (25.5).
+    // row blocks of all requests first: 6 x 2,534 queries, 3 heads 40.8 us (a request
+    // after another 49.8), 12 x 700, 8 heads 26.3 (31.9); short prompts with one tile take
+    // either way the same.
     int item = SPLIT ? blockIdx.x / a.split : blockIdx.x;
     const int rank = SPLIT ? blockIdx.x % a.split : 0;
     int g0 = 0, in_group = a.heads;
@@ -122,9 +121,8 @@ k_prefill(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap m_
         g0 = g * a.heads / a.groups, in_group = (g + 1) * a.heads / a.groups - g0;
         item -= g0 * per_head;
     }
-    const int rest = item / in_group, h = g0 + item - rest * in_group, beside = TILES == 2 ? a.requests : a.row_blocks;
-    const int outer = rest / beside, inner = rest - outer * beside;
-    const int b = TILES == 2 ? inner : outer, base = (a.row_blocks - 1 - (TILES == 2 ? outer : inner)) * TILES * kRows;
+    const int rest = item / in_group, h = g0 + item - rest * in_group, outer = rest / a.requests;
+    const int b = rest - outer * a.requests, base = (a.row_blocks - 1 - outer) * TILES * kRows;
     const int q0 = min(max(a.q_offsets[b], 0), a.q_rows), q1 = min(a.q_offsets[b + 1], a.q_rows);
     int k0 = min(max(a.k_offsets[b], 0), a.k_rows);
     const int k1 = min(a.k_offsets[b + 1], a.k_rows);
@@ -622,9 +620,9 @@ extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *str
     k.negative = a->scale < 0;
     const int64_t longest = a->longest < a->q_rows ? a->longest : a->q_rows;
     // One tile a block where most prompts leave the second one empty and keys
-    // are few: 37 ragged prompts up to 300, 16 heads 23.2 us (two tiles 31.1), 64 x 128
-    // tokens, 64 heads 129 us (189); two tiles for the rest: 37 x 512 tokens 98.8 us (one
-    // 113), 16 x 256 tokens after up to 1,000 cached ones 76 us (91).
+    // are few: 37 ragged prompts up to 300, 16 heads 24.8 us (two tiles 32.7), 64 x 128
+    // tokens, 64 heads 133 us (197); two tiles for the rest: 37 x 512 tokens 102 us (one
+    // 122), 16 x 256 tokens after up to 1,000 cached ones 77.5 us (96).
     const int tiles = longest <= 384 && a->q_rows <= 192 * (int64_t)a->requests && a->k_rows <= 384 * (int64_t)a->requests ? 1 : 2;
     k.row_blocks = (int)((longest + tiles * kRows - 1) / (tiles * kRows));
     // Heads side by side: as many as keep their keys and values within about a third of L2.
@@ -633,11 +631,11 @@ extern "C" int sim_op_latent_prefill(const sim_op_latent_prefill_t *a, void *str
     k.groups = (int)(fit < 1 ? a->heads : (a->heads + fit - 1) / fit);  // of equal size, or one apart: a last group of few heads would leave a long tail
     // Keys are split where blocks would leave half of the SMs empty, by as much as
     // keeps all blocks resident (of clusters of 8 there is room for fewer than 16).
-    // 16 heads of 1,000 queries after 2,728 cached tokens: 50.4 us, two stretches 35.8
-    // (four 45.5); 16 heads of 200 after 1,033: 21.4, two 19.2, four 16.0 (eight 28.0); 4 x
-    // 2,048: 29.4, four 18.2; 4 heads of 200 after 1,100: 22.0, four 15.1, eight 14.8.  The
-    // join takes 3 to 5 us, most where two blocks do it: 16 x 1,024 queries alone 18.4, two 18.6;
-    // 16 heads of 200 after 216: 12.2, four 12.0; after 97: 10.9, four 11.8.
+    // 16 heads of 1,000 queries after 2,728 cached tokens: 51.7 us, two stretches 36.3
+    // (four 46.5); 16 heads of 200 after 1,033: 22.2, two 20.1, four 16.8 (eight 29.2); 4 x
+    // 2,048: 30.1, four 19.1; 4 heads of 200 after 1,100: 22.7, four 15.7, eight 15.4.  The
+    // join takes 3 to 5 us, most where two blocks do it: 16 x 1,024 queries alone 19.1, two 19.3;
+    // 16 heads of 200 after 216: 13.0, four 13.1; after 97: 11.5, four 12.7.
     const int sms = sm_count();
     if (!sms) return SIM_ERR_CUDA;
     k.split = 1;
