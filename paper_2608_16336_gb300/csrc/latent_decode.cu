@@ -24,9 +24,9 @@ namespace {
 // a request: such pieces leave their sums in the workspace and k_join adds them.
 //
 // Bound by memory with one row tile: 3 requests of 90,001 to 130,000 tokens (406 MB)
-// take 91.6 us, 4.4 TB/s, of which 20 us are start, end and join.  Bound by the
+// take 91.8 us, 4.4 TB/s, of which 20 us are start, end and join.  Bound by the
 // chain from scores to sums with more: 64 requests of 200 to 10,240 tokens, 128
-// heads take 104 us, 480 TFLOP/s (218 MB of cache would take 33 us to read).
+// heads take 105 us, 478 TFLOP/s (218 MB of cache would take 33 us to read).
 constexpr int kRows = 64;
 constexpr int kRowBlockBytes = kRows * 128;  // 64 rows of 64 elements
 constexpr int kMaxBlocks = 9;                // 64-element column blocks of a row
@@ -86,7 +86,7 @@ __device__ __forceinline__ int tiles_of(const Args &a, int b) { return (tokens_o
 // Parts in use (each has a tile at least) and where one begins on the line.
 // As many parts as blocks and tiles allow; of few requests only so many that the
 // join, whose time grows with the pieces of a row, does not outweigh the tiles
-// saved (16 heads, 1 request of 8,000 tokens 22.1 us, with a part a block 26.6; of 3,000 17.8, 20.1).
+// saved (16 heads, 1 request of 8,000 tokens 22.0 us, with a part a block 26.0; of 3,000 17.8, 20.4).
 __device__ __forceinline__ int parts_of(const Args &a, int total) {
     return max(1, min(a.lanes, min(total, (int)(5.f * __fsqrt_rn((float)total * a.requests)))));
 }
@@ -699,8 +699,8 @@ template <typename T> int run(const Args &k, const CUtensorMap &m_cache, const C
     cudaError_t e = launch_early(kernel, c.row_tiles * c.lanes, kThreads, kShared, 1, st, k, m_cache, m_q);
     if (e != cudaSuccess) return launched("sim_op_latent_decode", e);
     // Few rows: a block shares the pieces of one; many: a warp has a row of its
-    // own.  2 x 128 heads 27.3 us (a warp a row 54.5), 8 x 128 30.4 (44.5), 64 x 16 60.2
-    // (60.8); a warp a row for 16 x 128 heads 48.3 (a block 48.6), 64 x 128 104 (130).
+    // own.  2 x 128 heads 27.2 us (a warp a row 54.7), 8 x 128 31.8 (45.0), 64 x 16 59.6
+    // (59.9); a warp a row for 16 x 128 heads 49.7 (a block 50.1), 64 x 128 100 (127).
     const int64_t rows = (int64_t)k.requests * k.new_tokens * k.heads;
     const bool few = rows <= 1024;
     const int64_t per = few ? 1 : kJoinWarps;
@@ -784,8 +784,8 @@ extern "C" int sim_op_latent_decode(const sim_op_latent_decode_t *a, void *strea
     auto stages_of = [&](int tile) { return (kShared - kRowBlockBytes - 1024 - col_blocks * k.q_pad * 128) / (col_blocks * tile * 128); };
     // Tiles of 64 tokens, whose scores take 1,208 cycles (of 32: 960).  Where only two
     // stages of 64 fit and one row tile leaves time to spare, five of 32 keep more
-    // in flight: 3 x 90,001 to 130,000 tokens, rank 512 91.7 us, with 64 93.7.  Rank 384 70.3 us,
-    // with 32 82.9; rank 256 54.1 (74.2); 64 requests of rank 512, 128 heads 104.2 (105.8).
+    // in flight: 3 x 90,001 to 130,000 tokens, rank 512 91.8 us, with 64 94.8.  Rank 384 68.7 us,
+    // with 32 76.9; rank 256 59.2 (75.7); 64 requests of rank 512, 128 heads 105.5 (112).
     k.tile = c.row_tiles == 1 && stages_of(64) < 3 ? 32 : 64;
     k.stages = stages_of(k.tile);
     if (k.stages > kMostStages) k.stages = kMostStages;

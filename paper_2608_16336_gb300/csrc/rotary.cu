@@ -7,7 +7,9 @@
 namespace mtop {
 namespace {
 
-// Any strides and offsets, an element at a time.
+// Any strides and offsets, an element at a time.  Bound by instructions, a 64-bit
+// division an element among them: 8,192 tokens x 128 heads of 192 an element off a
+// vector's place take 451 us (whole vectors 121), 1,000 x 16 heads 10.6 (6.0).
 template <typename T>
 __global__ void __launch_bounds__(256) k_rotary(sim_op_rotary_t a) {
     __shared__ float2 turn[SIM_OP_MAX_ROT / 2];
@@ -160,7 +162,8 @@ __global__ void __launch_bounds__(kGroupThreads, kGroupBlocks) k_rotary_wide(con
     }
 }
 
-// Any strides and sizes, an element at a time.
+// Any strides and sizes, an element at a time: 20,011 rows an element off a vector's
+// place 22.6 us (whole vectors 14.5; the host's slices included).
 template <typename T>
 __global__ void __launch_bounds__(128) k_append(sim_op_latent_append_t a) {
     const int half = a.rot_dim / 2;

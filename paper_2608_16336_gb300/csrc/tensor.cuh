@@ -201,6 +201,8 @@ __device__ __forceinline__ void cluster_sync() {
 }
 
 // ------------------------------------------------------------ arithmetic --
+// 2^x to about 2^-22 of itself, results below 2^-126 as 0: finer than the
+// weights are rounded (2^-9, 2^-12), and one instruction where the full function is several.
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -163,8 +163,10 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, *, scaling: str | No
     so that the slowest pair is slowed by ``factor`` and the fastest by nothing;
     ``"ramp"`` keeps the pairs that turn more than ``fast`` times over the
     ``trained`` length, divides those that turn less than ``slow`` times by
-    ``factor``, and goes linearly from one to the other in between (use it with
-    ``amplitude=ramp_amplitude(factor)``)."""
+    ``factor``, and goes linearly in the number of turns from one to the other in
+    between (use it with ``amplitude=ramp_amplitude(factor)``).  A model whose ramp
+    was linear in the pair's index, or had its ends rounded to whole pairs, needs
+    the vector that it was trained with: any float64 vector of radians per position does."""
     if rot_dim < 2 or rot_dim % 2 or rot_dim > MAX_ROT:
         raise ValueError("rot_dim must be even and in [2, %d]" % MAX_ROT)
     if not base > 0 or not factor > 0:
