@@ -119,7 +119,7 @@ int sim_op_latent_append(const sim_op_latent_append_t *args, void *cuda_stream);
  *   s_j = scale * <q[b][t][h], c_j>   for j < L - new_tokens + 1 + t
  *   lse[b][t][h] = log sum_j exp s_j
  *   out[b][t][h] = sum_j exp(s_j - lse) c_j[0 .. rank)
- * A row that sees nothing gives zeros and lse = -infinity; one whose scores
+ * A row that sees nothing, or only scores of -infinity, gives zeros and lse = -infinity; one whose scores
  * are NaN or +infinity gives NaN.  lengths are taken
  * as at most table_blocks * T; a table entry outside [0, blocks) stands for a
  * block of zeros.  Cached rows from L on are never used, whatever they hold,
