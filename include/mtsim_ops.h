@@ -15,6 +15,13 @@
  *   sim_op_latent_prefill  causal attention with expanded keys and values
  *   sim_op_sample          temperature, top-k, top-p, min-p and the draw
  *
+ * The same over a cache of 8-bit numbers, for drafted tokens, and between caches:
+ *
+ *   sim_op_quantized_append  new tokens' rows into an 8-bit block cache with scales
+ *   sim_op_quantized_decode  attention of new tokens over such a cache
+ *   sim_op_verify            which drafted tokens the target's probabilities keep, and the next
+ *   sim_op_block_copy        blocks of all layers to other blocks (fork, migration, compaction)
+ *
  * Conventions for every entry point:
  *  - The argument struct is host memory and may be reused when the call
  *    returns; every pointer inside it is device memory of the current device,
@@ -60,6 +67,7 @@ extern "C" {
 #define SIM_OP_MAX_KEY 64       /* elements of the shared rotated key of attention */
 #define SIM_OP_MAX_HEAD 128     /* elements of a head's own key part, and of its values */
 #define SIM_OP_MAX_VOCAB (1 << 20)
+#define SIM_OP_MAX_DRAFTS 64    /* drafted tokens of a request */
 
 /* Rotary positions.  With d = rot_dim, o = rot_offset, p = positions[n] and
  * the pairs (a, b) of x[n][h][o .. o+d):
@@ -223,6 +231,141 @@ typedef struct {
 } sim_op_sample_t;
 
 int sim_op_sample(const sim_op_sample_t *args, void *cuda_stream);
+
+/* The 8-bit block cache.  A cached number is an e4m3 float (four significant
+ * bits, largest 448, multiples of 2^-9) times a scale; a block has two scales, for the latent
+ * part (elements [0, rank)) and for the rotated key part, at scales[block][0] and [1].
+ *
+ * Appends the new tokens of ragged requests.  Request b's are rows
+ * [offsets[b], offsets[b+1]) of latent and key, n of them, and become its cached tokens
+ * lengths[b] - n .. lengths[b] - 1 (lengths counts cached tokens, the new ones
+ * included; a token's index is its rotary position).  Token p is row p % T of block table[b][p / T]:
+ * [latent, rotated key (as above, with amplitude)], divided by the block's scales and
+ * rounded to the nearest e4m3 (ties to even).  Nothing is rounded before that.
+ * A block's scales come from what is written.  need = the smallest power of
+ * two in [2^-60, 2^60] with max |x| <= 448 * need over the rows of this call in
+ * the block.  Where row 0 is among them the block begins anew and its scale is need;
+ * else it is the larger of need and the scale it had, and if need is larger, the rows before
+ * the first written one are expressed in the new scale (exactly, where both are
+ * powers of two, but for numbers below 2^-6 of it, rounded to the nearest).
+ * Infinities and NaN are stored as NaN and have no part in the scale; numbers beyond 448 * 2^60 as +-448.
+ * Rows of the block after the last written one are left as they were (with another scale: they are no cached tokens).
+ * Offsets must not decrease and are bounded by tokens; rows that belong to no
+ * request, tokens with an index below 0 or past the table's end and table entries outside [0, blocks)
+ * write nothing.  Two requests of one call must not write the same block. */
+typedef struct {
+    const void *latent;         /* [tokens][rank] */
+    const void *key;            /* [tokens][rot_dim] */
+    const double *frequencies;  /* [rot_dim / 2] */
+    const int32_t *offsets;     /* [requests + 1] */
+    const int32_t *table;       /* [requests][table_blocks], rows `table_row` apart */
+    const int32_t *lengths;     /* [requests] */
+    void *cache;                /* [blocks][block_tokens][rank + rot_dim], e4m3 */
+    float *scales;              /* [blocks][2], contiguous */
+    int64_t tokens;
+    int64_t latent_token, key_token; /* strides */
+    int64_t cache_block, cache_row, table_row;
+    int64_t blocks;
+    int32_t requests, table_blocks;
+    int32_t block_tokens;       /* T >= 1 */
+    int32_t rank, rot_dim;      /* rank >= 1, any; rot_dim even, at most SIM_OP_MAX_ROT */
+    int32_t type, layout;       /* of latent and key */
+    float amplitude;
+} sim_op_quantized_append_t;
+
+int sim_op_quantized_append(const sim_op_quantized_append_t *args, void *cuda_stream);
+
+/* sim_op_latent_decode over an 8-bit cache: cached row j is [a c_j, b c'_j] with the
+ * scales a, b of its block, and
+ *   s_j = scale * (a <q[0 .. rank), c_j> + b <q[rank ..), c'_j>)
+ *   out = sum_j exp(s_j - lse) a c_j
+ * Scales are positive; one outside [2^-60, 2^60] is taken as the nearer end, NaN as 2^-60.  NaN in a cached row makes the
+ * rows that see it NaN, in a query its own row (an infinity in a query counts as NaN).  Lengths, table entries and rows
+ * past a request's tokens are treated as there.
+ * The numbers of the cache are used as they are.  Queries and weights exp(s - max)
+ * are rounded for the products: a query's elements by nothing, or by at most 2^-21 of its largest;
+ * each weight by at most 2^-9 (bfloat16 calls) or 2^-12 (float16 calls) of itself, one
+ * far below the largest (weight times a) by at most 2^-32 of that.  Sums, scores and statistics are in 32 bits, lse's sum is of the unrounded weights.
+ * type is q's and out's: 16-bit.  Alignment: pointers and q's and out's strides in multiples of 16
+ * bytes (8 elements); cache strides and key_dim in multiples of 16; rank a multiple of 64;
+ * cache_block is a multiple of cache_row.  workspace: as there, sim_op_quantized_decode_workspace() bytes. */
+typedef struct {
+    const void *q;              /* [requests][new_tokens][heads][rank + key_dim] */
+    const void *cache;          /* [blocks][block_tokens][rank + key_dim], e4m3 */
+    const float *scales;        /* [blocks][2], contiguous */
+    const int32_t *table;       /* [requests][table_blocks], rows `table_row` apart */
+    const int32_t *lengths;     /* [requests] */
+    void *out;                  /* [requests][new_tokens][heads][rank] */
+    float *lse;                 /* [requests][new_tokens][heads], contiguous, or NULL */
+    void *workspace;
+    size_t workspace_bytes;
+    int64_t q_request, q_token, q_head; /* strides */
+    int64_t out_request, out_token, out_head;
+    int64_t cache_block, cache_row, table_row;
+    int64_t blocks;
+    int32_t requests, new_tokens, heads;
+    int32_t rank, key_dim;
+    int32_t block_tokens, table_blocks;
+    int32_t type;
+    float scale;
+} sim_op_quantized_decode_t;
+
+int sim_op_quantized_decode(const sim_op_quantized_decode_t *args, void *cuda_stream);
+size_t sim_op_quantized_decode_workspace(int32_t requests, int32_t new_tokens, int32_t heads, int32_t rank);
+
+/* Verification of drafted tokens.  Request b has D = drafted[b] of them (at most
+ * `drafts`; NULL: all have `drafts`), the target's logits for the token after each (row
+ * 0: in the first one's place, row D: after the last) and the logits that the drafted ones were drawn from.
+ * With t the temperature, p_i = softmax(target_i / t) and q_i = softmax(draft_i / t):
+ *   1. drafted tokens x_0, x_1, .. are accepted while uniform[i] * q_i(x_i) < p_i(x_i);
+ *   2. at the first that is not, i, the next token is drawn from max(p_i - q_i, 0)
+ *      scaled to a sum of one (where that is 0 everywhere: from p_i); with all accepted, from p_D;
+ *   3. the draw takes the first token, in vocabulary order, up to which the weights sum to more
+ *      than uniform[drafts] times their total.
+ * So the tokens are distributed as if drawn from the target one by one.  out[b] holds
+ * the accepted tokens, the drawn one, and -1 behind; count[b] how many tokens these are (accepted + 1);
+ * logprob[b][i] is log p_i of out[b][i] (-infinity behind).
+ * draft NULL: the drafted tokens were certain, q_i is 1 there and 0 elsewhere.
+ * A temperature that is not above zero makes p_i and q_i 1 at the largest logit (the lowest index of them) and 0 elsewhere.
+ * NaN logits count as -infinity; with +infinite logits the probability is shared
+ * by these.  In a row without a logit above -infinity every probability is 0: a drafted token is refused there, a draw
+ * gives -1 and -infinity.  A drafted token outside [0, vocab) has probability 0
+ * under both.  Weights exp((l - max) / t) are in 32 bits (one below 2^-126 is 0), sums over the vocabulary in 64. */
+typedef struct {
+    const void *target;         /* [requests][drafts + 1][vocab] */
+    const void *draft;          /* [requests][drafts][vocab], the target's type, or NULL */
+    const int64_t *tokens;      /* [requests][drafts] */
+    const float *uniform;       /* [requests][drafts + 1], in [0, 1) */
+    const float *temperature;   /* [requests] or NULL (1) */
+    const int32_t *drafted;     /* [requests] or NULL; taken as at least 0 and at most drafts */
+    int64_t *out;               /* [requests][drafts + 1] */
+    int32_t *count;             /* [requests] */
+    float *logprob;             /* [requests][drafts + 1] or NULL */
+    int64_t target_request, target_row, draft_request, draft_row; /* strides */
+    int32_t requests, drafts, vocab; /* drafts in [0, SIM_OP_MAX_DRAFTS], vocab in [1, SIM_OP_MAX_VOCAB] */
+    int32_t type;
+} sim_op_verify_t;
+
+int sim_op_verify(const sim_op_verify_t *args, void *cuda_stream);
+
+/* Copies blocks, in every layer: block to_blocks[i] of destination becomes block
+ * from_blocks[i] of source, for all i.  The tensors are a cache or what belongs to one (scales): a block
+ * of a layer is `rows` rows of row_bytes bytes.  A pair with either number outside its
+ * tensor's blocks copies nothing (padding).  destination may be source, or overlap it, when no block that is
+ * written is read by another pair; no two pairs may have the same destination.  Strides are in bytes. */
+typedef struct {
+    const void *source;         /* [layers][source_blocks][rows][row_bytes] */
+    void *destination;          /* [layers][destination_blocks][rows][row_bytes] */
+    const int32_t *from_blocks; /* [pairs] */
+    const int32_t *to_blocks;   /* [pairs] */
+    int64_t row_bytes;
+    int64_t source_layer, source_block, source_row;
+    int64_t destination_layer, destination_block, destination_row;
+    int64_t source_blocks, destination_blocks;
+    int32_t layers, rows, pairs;
+} sim_op_block_copy_t;
+
+int sim_op_block_copy(const sim_op_block_copy_t *args, void *cuda_stream);
 
 /* Number of waits inside the operators' kernels that ran out of their limit
  * on the current device since the library was loaded: 0, unless a kernel is

@@ -4,7 +4,9 @@ The simulation charges an iteration a base time plus so much a prefill token
 and a decode request; the paper's simulator takes such times from operators
 profiled on a GPU (Sec. 2.5, 4.1).  These are the operators to profile, over
 the same kind of block-paged cache: ``rotary``, ``latent_append``,
-``latent_decode``, ``latent_prefill`` and ``sample``.  ``instance.py`` runs
+``latent_decode``, ``latent_prefill`` and ``sample``; ``quantized_append``
+and ``quantized_decode`` over a cache of 8-bit numbers with scales; ``verify`` for drafted
+tokens; ``block_copy`` for blocks that are forked, migrated or compacted.  ``instance.py`` runs
 them together as an instance would and fits the three times.
 
 Each function takes CUDA tensors of the current device and queues its kernels
@@ -31,7 +33,8 @@ from . import mtsim
 
 TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 LAYOUTS = {"interleaved": 0, "half": 1}
-MAX_ROT, MAX_RANK, MAX_KEY, MAX_HEAD, MAX_VOCAB = 256, 512, 64, 128, 1 << 20
+MAX_ROT, MAX_RANK, MAX_KEY, MAX_HEAD, MAX_VOCAB, MAX_DRAFTS = 256, 512, 64, 128, 1 << 20, 64
+EIGHT = torch.float8_e4m3fn  # of the 8-bit cache
 
 # The argument structs in the C compiler's layout (native alignment).  Packing
 # 20 fields takes a fifth of the time of filling a ctypes structure, and small
@@ -41,12 +44,18 @@ APPEND = Struct("@PPPPPPqqqqqqiiiiiif0q")
 DECODE = Struct("@PPPPPPPNqqqqqqqqqqiiiiiiiif0q")
 PREFILL = Struct("@PPPPPPPPqqqqqqqqqqqiiiiiiiif0q")
 SAMPLE = Struct("@PPPPPPPPqiii0q")
+QUANTIZED_APPEND = Struct("@PPPPPPPPqqqqqqqiiiiiiif0q")
+QUANTIZED_DECODE = Struct("@PPPPPPPPNqqqqqqqqqqiiiiiiiif0q")
+VERIFY = Struct("@PPPPPPPPPqqqqiiii0q")
+BLOCK_COPY = Struct("@PPPPqqqqqqqqqiii0q")
 
 EXPORTS = ["sim_op_rotary", "sim_op_latent_append", "sim_op_latent_decode", "sim_op_latent_decode_workspace",
-           "sim_op_latent_prefill", "sim_op_sample", "sim_op_faults", "sim_op_last_error"]
+           "sim_op_latent_prefill", "sim_op_sample", "sim_op_quantized_append", "sim_op_quantized_decode",
+           "sim_op_quantized_decode_workspace", "sim_op_verify", "sim_op_block_copy", "sim_op_faults", "sim_op_last_error"]
 
 _LIB = None
 _WORKSPACE: dict[tuple, int] = {}  # bytes by sizes
+_QUANTIZED_WORKSPACE: dict[tuple, int] = {}
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
@@ -62,11 +71,12 @@ def lib() -> ctypes.CDLL:
     global _LIB
     if _LIB is None:
         L = mtsim.lib()
-        for name in ("rotary", "latent_append", "latent_decode", "latent_prefill", "sample"):
+        for name in ("rotary", "latent_append", "latent_decode", "latent_prefill", "sample", "quantized_append", "quantized_decode",
+                     "verify", "block_copy"):
             f = getattr(L, "sim_op_" + name)
             f.argtypes, f.restype = [ctypes.c_char_p, ctypes.c_void_p], ctypes.c_int
-        L.sim_op_latent_decode_workspace.argtypes = [ctypes.c_int32] * 4
-        L.sim_op_latent_decode_workspace.restype = ctypes.c_size_t
+        for f in (L.sim_op_latent_decode_workspace, L.sim_op_quantized_decode_workspace):
+            f.argtypes, f.restype = [ctypes.c_int32] * 4, ctypes.c_size_t
         L.sim_op_faults.argtypes, L.sim_op_faults.restype = [], ctypes.c_int
         L.sim_op_last_error.argtypes, L.sim_op_last_error.restype = [], ctypes.c_char_p
         _LIB = L
@@ -127,6 +137,24 @@ def _rows(name, t, shape):
     if s[-1] != 1 and shape[-1] > 1:
         raise ValueError("the last dimension of %s must be contiguous" % name)
     return s
+
+
+def _int32(name, t, shape) -> None:
+    if t.dtype is not torch.int32:
+        raise TypeError("%s must be int32, not %s" % (name, t.dtype))
+    _packed(name, t, shape)
+
+
+def _eight(cache, scales, width) -> tuple:
+    """The strides of an 8-bit cache with its scales."""
+    if cache.dtype is not EIGHT:
+        raise TypeError("cache must be float8_e4m3fn, not %s" % cache.dtype)
+    if scales.dtype is not torch.float32:
+        raise TypeError("scales must be float32, not %s" % scales.dtype)
+    if cache.dim() != 3:
+        raise ValueError("cache must be [blocks, block_tokens, width]")
+    _packed("scales", scales, (cache.shape[0], 2))
+    return _rows("cache", cache, (cache.shape[0], cache.shape[1], width))
 
 
 def _positions(t, n) -> int:
@@ -389,3 +417,186 @@ def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=N
         _failed(rc)
     _changed((out, logprob))
     return out, logprob
+
+
+def quantized_append(latent, key, frequencies, offsets, table, lengths, cache, scales, *, layout="interleaved", amplitude=1.0):
+    """Writes the new tokens of ragged requests into an 8-bit block cache:
+    ``cache`` float8_e4m3fn [blocks, block_tokens, rank + rot] with ``scales``
+    float32 [blocks, 2], one for a block's latent part and one for its rotated
+    key part (powers of two; a cached number is their product).  Request b's
+    tokens are the rows between ``offsets[b]`` and ``[b + 1]`` (int32) of
+    ``latent`` [tokens, rank] and ``key`` [tokens, rot]; they become its last
+    cached ones, ``lengths[b]`` (int32) counting these with them, in the
+    blocks that ``table`` int32 [requests, n] names.  A token's index is its
+    rotary position.  A block whose first row is written begins anew; one that
+    holds rows keeps them, in a larger scale where the new rows need one.
+    Returns (cache, scales)."""
+    rot = _frequencies(frequencies)
+    if latent.dim() != 2 or table.dim() != 2:
+        raise ValueError("latent must be [tokens, rank], table [requests, n]")
+    n, rank = latent.shape
+    b, width = table.shape
+    ls, ks = _rows("latent", latent, latent.shape), _rows("key", key, (n, rot))
+    cs = _eight(cache, scales, rank + rot)
+    _int32("offsets", offsets, (b + 1,))
+    _int32("lengths", lengths, (b,))
+    if table.dtype is not torch.int32:
+        raise TypeError("table must be int32, not %s" % table.dtype)
+    ts = _rows("table", table, (b, width))
+    code = _type("latent", latent, key)
+    device = _place(latent, key, cache, scales, frequencies, offsets, table, lengths)
+    rc = (_LIB or lib()).sim_op_quantized_append(
+        QUANTIZED_APPEND.pack(latent.data_ptr(), key.data_ptr(), frequencies.data_ptr(), offsets.data_ptr(), table.data_ptr(),
+                              lengths.data_ptr(), cache.data_ptr(), scales.data_ptr(), n, ls[0], ks[0], cs[0], cs[1], ts[0],
+                              cache.shape[0], b, width, cache.shape[1], rank, rot, code, _layout(layout), amplitude),
+        _stream_of(device))
+    if rc:
+        _failed(rc)
+    _changed((cache, scales))
+    return cache, scales
+
+
+def quantized_decode(q, cache, scales, table, lengths, *, scale, out=None, lse=None):
+    """``latent_decode`` over an 8-bit cache as ``quantized_append`` fills it:
+    ``cache`` float8_e4m3fn [blocks, block_tokens, width], ``scales`` float32
+    [blocks, 2].  Returns (out [requests, new, heads, rank] in q's type, lse float32)."""
+    if q.dim() != 4 or table.dim() != 2:
+        raise ValueError("q must be [requests, new, heads, width], table [requests, n]")
+    b, new, heads, width = q.shape
+    if out is None:
+        out = torch.empty((b, new, heads, width - 64), dtype=q.dtype, device=q.device)
+    rank = out.shape[-1]
+    if rank < 64 or rank > MAX_RANK or rank % 64 or not 0 <= width - rank <= MAX_KEY or width % 16:
+        raise ValueError("rank must be a multiple of 64 up to %d and width - rank one of 16 up to %d: %d, %d"
+                         % (MAX_RANK, MAX_KEY, rank, width - rank))
+    qs, os_ = _rows("q", q, q.shape), _rows("out", out, (b, new, heads, rank))
+    cs = _eight(cache, scales, width)
+    if table.dtype is not torch.int32:
+        raise TypeError("table must be int32, not %s" % table.dtype)
+    ts = _rows("table", table, (b, table.shape[1]))
+    _int32("lengths", lengths, (b,))
+    if lse is None:
+        lse = torch.empty((b, new, heads), dtype=torch.float32, device=q.device)
+    elif lse.dtype is not torch.float32:
+        raise TypeError("lse must be float32")
+    _packed("lse", lse, (b, new, heads))
+    code = _type("q", q, out, wide=False)
+    device = _place(q, cache, scales, out, lse, table, lengths)
+    L = _LIB or lib()
+    size = (device, b, new, heads, rank)
+    nbytes = _QUANTIZED_WORKSPACE.get(size)
+    if nbytes is None:
+        nbytes = L.sim_op_quantized_decode_workspace(b, new, heads, rank)
+        if not nbytes:  # the device could not be asked: not an answer to keep
+            _failed(mtsim.SIM_ERR_CUDA)
+        _QUANTIZED_WORKSPACE[size] = nbytes
+    stream = _stream_of(device)
+    work = _scratch(nbytes, stream)
+    try:
+        rc = L.sim_op_quantized_decode(
+            QUANTIZED_DECODE.pack(q.data_ptr(), cache.data_ptr(), scales.data_ptr(), table.data_ptr(), lengths.data_ptr(), out.data_ptr(),
+                                  lse.data_ptr(), work, nbytes, qs[0], qs[1], qs[2], os_[0], os_[1], os_[2], cs[0], cs[1], ts[0],
+                                  cache.shape[0], b, new, heads, rank, width - rank, cache.shape[1], table.shape[1], code, scale),
+            stream)
+    finally:
+        _release(work)  # what the stream allocates next comes after this call's kernels
+    if rc:
+        _failed(rc)
+    _changed((out, lse))
+    return out, lse
+
+
+def verify(target, tokens, uniform, *, draft=None, temperature=None, drafted=None, out=None, count=None, logprob=None):
+    """Which drafted tokens the target keeps, and the token after them.
+    ``target`` [requests, drafts + 1, vocab] are the target's logits in the
+    place of each drafted token and after the last, ``tokens`` int64 [requests,
+    drafts] the drafted ones and ``draft`` [requests, drafts, vocab] the logits
+    that they were drawn from (None: they were certain).  Token i is accepted while
+    ``uniform[:, i]`` times its probability in the draft is below that in the
+    target; the next is drawn by ``uniform[:, drafts]`` from what the target
+    has more than the draft at the first refusal, or after the last token.
+    ``uniform`` is float32 [requests, drafts + 1] in [0, 1), ``temperature``
+    float32 [requests] (zero: the largest logit) of both, ``drafted`` int32
+    [requests] how many tokens a request has (None: all have ``drafts``).
+    Logits that a limit or a grammar rules out are -infinity.  Returns (out int64 [requests, drafts + 1], -1
+    behind the drawn token; count int32 [requests], accepted + 1; logprob
+    float32 [requests, drafts + 1], the target's)."""
+    if target.dim() != 3:
+        raise ValueError("target must be [requests, drafts + 1, vocab]")
+    b, places, vocab = target.shape
+    d = places - 1
+    if not 0 <= d <= MAX_DRAFTS:
+        raise ValueError("target must have 1 to %d rows a request (drafted tokens and one), not %d" % (MAX_DRAFTS + 1, places))
+    if not 1 <= vocab <= MAX_VOCAB:
+        raise ValueError("a vocabulary has 1 to %d tokens, not %d" % (MAX_VOCAB, vocab))
+    rs = _rows("target", target, target.shape)
+    code = _type("target", target)
+    if tokens.dtype is not torch.int64 or uniform.dtype is not torch.float32:
+        raise TypeError("tokens must be int64 and uniform float32, not %s and %s" % (tokens.dtype, uniform.dtype))
+    _packed("tokens", tokens, (b, d))
+    _packed("uniform", uniform, (b, places))
+    used = [target, tokens, uniform]
+    ds = (0, 0)
+    if draft is not None:
+        _type("target", target, draft)
+        ds = _rows("draft", draft, (b, d, vocab))
+        used.append(draft)
+    for name, t, dtype in (("temperature", temperature, torch.float32), ("drafted", drafted, torch.int32)):
+        if t is not None:
+            if t.dtype is not dtype:
+                raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
+            _packed(name, t, (b,))
+            used.append(t)
+    if out is None:
+        out = torch.empty((b, places), dtype=torch.int64, device=target.device)
+    if count is None:
+        count = torch.empty(b, dtype=torch.int32, device=target.device)
+    if logprob is None:
+        logprob = torch.empty((b, places), dtype=torch.float32, device=target.device)
+    if out.dtype is not torch.int64 or count.dtype is not torch.int32 or logprob.dtype is not torch.float32:
+        raise TypeError("out must be int64, count int32 and logprob float32")
+    _packed("out", out, (b, places))
+    _packed("count", count, (b,))
+    _packed("logprob", logprob, (b, places))
+    device = _place(*used, out, count, logprob)
+    rc = (_LIB or lib()).sim_op_verify(
+        VERIFY.pack(target.data_ptr(), 0 if draft is None else draft.data_ptr(), tokens.data_ptr(), uniform.data_ptr(),
+                    0 if temperature is None else temperature.data_ptr(), 0 if drafted is None else drafted.data_ptr(), out.data_ptr(),
+                    count.data_ptr(), logprob.data_ptr(), rs[0], rs[1], ds[0], ds[1], b, d, vocab, code),
+        _stream_of(device))
+    if rc:
+        _failed(rc)
+    _changed((out, count, logprob))
+    return out, count, logprob
+
+
+def block_copy(source, destination, from_blocks, to_blocks):
+    """Copies blocks in every layer: ``destination[:, to_blocks[i]]`` becomes
+    ``source[:, from_blocks[i]]``.  Both are [layers, blocks, block_tokens,
+    width] or [layers, blocks, width] (a cache, its scales) of any type,
+    ``from_blocks`` and ``to_blocks`` int32 vectors on the device; a pair with a
+    number outside its tensor's blocks (-1: padding) copies nothing.  They may be one tensor when no
+    block that is written is read by another pair; no two pairs may name the same
+    destination.  Returns ``destination``."""
+    if source.dim() not in (3, 4) or source.dim() != destination.dim():
+        raise ValueError("source and destination must be [layers, blocks, block_tokens, width] or [layers, blocks, width]")
+    if source.dtype is not destination.dtype:
+        raise TypeError("source and destination must have the same type: %s and %s" % (source.dtype, destination.dtype))
+    layers, have, *block = source.shape
+    room = destination.shape[1]
+    ss, ds = _rows("source", source, source.shape), _rows("destination", destination, (layers, room, *block))
+    n = from_blocks.shape[0] if from_blocks.dim() == 1 else -1
+    if n < 0:
+        raise ValueError("from_blocks must be a vector")
+    _int32("from_blocks", from_blocks, (n,))
+    _int32("to_blocks", to_blocks, (n,))
+    device = _place(source, destination, from_blocks, to_blocks)
+    e, rows = source.element_size(), block[0] if len(block) == 2 else 1
+    rc = (_LIB or lib()).sim_op_block_copy(
+        BLOCK_COPY.pack(source.data_ptr(), destination.data_ptr(), from_blocks.data_ptr(), to_blocks.data_ptr(), block[-1] * e,
+                        ss[0] * e, ss[1] * e, ss[2] * e, ds[0] * e, ds[1] * e, ds[2] * e, have, room, layers, rows, n),
+        _stream_of(device))
+    if rc:
+        _failed(rc)
+    _changed((destination,))
+    return destination
