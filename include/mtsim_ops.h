@@ -284,8 +284,8 @@ int sim_op_quantized_append(const sim_op_quantized_append_t *args, void *cuda_st
  * past a request's tokens are treated as there.
  * The numbers of the cache are used as they are.  Queries and weights exp(s - max)
  * are rounded for the products: a query's elements by nothing, or by at most 2^-21 of its largest;
- * each weight by at most 2^-9 (bfloat16 calls) or 2^-12 (float16 calls) of itself, one
- * far below the largest (weight times a) by at most 2^-32 of that.  Sums, scores and statistics are in 32 bits, lse's sum is of the unrounded weights.
+ * each weight by at most 1.25 * 2^-9 (bfloat16 calls) or 1.5 * 2^-11 (float16 calls) of itself, one whose product with a is
+ * far below the request's largest by at most 2^-27 of that.  Sums, scores and statistics are in 32 bits, lse's sum is of the unrounded weights.
  * type is q's and out's: 16-bit.  Alignment: pointers and q's and out's strides in multiples of 16
  * bytes (8 elements); cache strides and key_dim in multiples of 16; rank a multiple of 64;
  * cache_block is a multiple of cache_row.  workspace: as there, sim_op_quantized_decode_workspace() bytes. */

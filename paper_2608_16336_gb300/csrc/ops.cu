@@ -50,7 +50,9 @@ bool allow_shared(const void *kernel, int bytes, std::atomic<uint64_t> &done) {
     return true;
 }
 
-bool box_map(CUtensorMap *map, const void *base, bool bf16, int dims, const uint64_t *size, const int64_t *stride, const uint32_t *box) {
+namespace {
+bool make_map(CUtensorMap *map, const void *base, CUtensorMapDataType type, int bytes, int dims, const uint64_t *size, const int64_t *stride,
+              const uint32_t *box) {
     static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> encode{nullptr};
     PFN_cuTensorMapEncodeTiled_v12000 f = encode.load(std::memory_order_acquire);
     if (!f) {
@@ -66,16 +68,25 @@ bool box_map(CUtensorMap *map, const void *base, bool bf16, int dims, const uint
     }
     cuuint64_t strides[4];
     cuuint32_t ones[5] = {1, 1, 1, 1, 1};
-    for (int d = 0; d + 1 < dims; ++d) strides[d] = (cuuint64_t)stride[d] * 2;
-    const CUresult r = f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)dims,
-                         const_cast<void *>(base), (const cuuint64_t *)size, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    for (int d = 0; d + 1 < dims; ++d) strides[d] = (cuuint64_t)stride[d] * bytes;
+    const CUresult r = f(map, type, (cuuint32_t)dims, const_cast<void *>(base), (const cuuint64_t *)size, strides, box, ones,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, box[0] * bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) fail(SIM_ERR_CUDA, "tensor map: driver error %d", (int)r);
     return r == CUDA_SUCCESS;
+}
+}  // namespace
+
+bool box_map(CUtensorMap *map, const void *base, bool bf16, int dims, const uint64_t *size, const int64_t *stride, const uint32_t *box) {
+    return make_map(map, base, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, dims, size, stride, box);
+}
+bool byte_box_map(CUtensorMap *map, const void *base, int dims, const uint64_t *size, const int64_t *stride, const uint32_t *box) {
+    return make_map(map, base, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, dims, size, stride, box);
 }
 
 unsigned decode_faults();
 unsigned prefill_faults();
+unsigned quantized_faults();
 
 }  // namespace mtop
 
@@ -83,8 +94,8 @@ extern "C" int sim_op_faults(void) {
     // (a copy alone would not wait for streams that do not wait for the default one)
     const cudaError_t e = cudaDeviceSynchronize();
     if (e != cudaSuccess) return mtop::launched("sim_op_faults", e);
-    const unsigned d = mtop::decode_faults(), p = mtop::prefill_faults(), n = d + p;
-    return d == ~0u || p == ~0u || n > 0x7FFFFFFFu ? mtop::fail(SIM_ERR_CUDA, "the fault counter cannot be read") : (int)n;
+    const unsigned d = mtop::decode_faults(), p = mtop::prefill_faults(), q = mtop::quantized_faults(), n = d + p + q;
+    return d == ~0u || p == ~0u || q == ~0u || n > 0x7FFFFFFFu ? mtop::fail(SIM_ERR_CUDA, "the fault counter cannot be read") : (int)n;
 }
 
 extern "C" const char *sim_op_last_error(void) { return mtop::t_error; }

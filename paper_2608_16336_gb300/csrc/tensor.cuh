@@ -57,6 +57,15 @@ __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, bool &de
     atomicAdd(&g_faults, 1u);
 }
 
+// The same in less code, for kernels whose warps do different things: what they
+// run between waits is bound by fetching it.
+__device__ __forceinline__ void bar_await(uint32_t bar, uint32_t parity, bool &dead) {
+    int i = 0;
+#pragma unroll 1
+    while (!bar_test(bar, parity) && !dead)
+        if (++i == kWaitLimit) dead = true, atomicAdd(&g_faults, 1u);
+}
+
 // ---------------------------------------------------------- bulk copies ---
 __device__ __forceinline__ void copy_box_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
     asm volatile(
@@ -280,6 +289,8 @@ __device__ __forceinline__ float below_top(float x, float scale, float top) {
 // elements in 128-byte-swizzled boxes; false with the error set when the
 // driver refuses it.  strides: elements, of dimensions 1 and up.
 bool box_map(CUtensorMap *map, const void *base, bool bf16, int dims, const uint64_t *size, const int64_t *stride, const uint32_t *box);
+// The same of bytes; a box 64 of them wide is swizzled within its rows.
+bool byte_box_map(CUtensorMap *map, const void *base, int dims, const uint64_t *size, const int64_t *stride, const uint32_t *box);
 
 }  // namespace mtop
 

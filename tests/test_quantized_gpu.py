@@ -5,7 +5,7 @@ Tolerances, from the arithmetic.  A number stored in 8 bits (four significant bi
 most half its step, 2^-4 of itself or 2^-10, and a rotated key by what 32 bits leave
 (2e-6 of the pair's length, which may also tip a rounding); latents are rounded once and
 compared exactly.  An attention's result of unit roundoff u / 2 (bfloat16: u = 2^-8) is off by u / 2 |y| for its own rounding, u / 2 sum_j p_j |v_j|
-for the weights' (a weight is rounded by 2^-9 or 2^-12 of itself); twice that is allowed, and 1e-5 of the same sum for 32-bit
+for the weights' (a weight is rounded by 1.25 * 2^-9 or 1.5 * 2^-11 of itself); twice that is allowed, and 1e-5 of the same sum for 32-bit
 arithmetic.  A query's elements may be off by 2^-21 of its largest, so that a
 score is by 2^-21 max |q| sum |c| |scale|, its weight by twice that, and lse by as much."""
 import math
