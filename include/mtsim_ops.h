@@ -341,12 +341,15 @@ typedef struct {
     int64_t *out;               /* [requests][drafts + 1] */
     int32_t *count;             /* [requests] */
     float *logprob;             /* [requests][drafts + 1] or NULL */
+    void *workspace;            /* sim_op_verify_workspace() bytes, 256-byte aligned, not to be shared by calls that overlap */
+    size_t workspace_bytes;
     int64_t target_request, target_row, draft_request, draft_row; /* strides */
     int32_t requests, drafts, vocab; /* drafts in [0, SIM_OP_MAX_DRAFTS], vocab in [1, SIM_OP_MAX_VOCAB] */
     int32_t type;
 } sim_op_verify_t;
 
 int sim_op_verify(const sim_op_verify_t *args, void *cuda_stream);
+size_t sim_op_verify_workspace(int32_t requests, int32_t drafts, int32_t with_draft, int32_t vocab);
 
 /* Copies blocks, in every layer: block to_blocks[i] of destination becomes block
  * from_blocks[i] of source, for all i.  The tensors are a cache or what belongs to one (scales): a block

@@ -46,16 +46,17 @@ PREFILL = Struct("@PPPPPPPPqqqqqqqqqqqiiiiiiiif0q")
 SAMPLE = Struct("@PPPPPPPPqiii0q")
 QUANTIZED_APPEND = Struct("@PPPPPPPPqqqqqqqiiiiiiif0q")
 QUANTIZED_DECODE = Struct("@PPPPPPPPNqqqqqqqqqqiiiiiiiif0q")
-VERIFY = Struct("@PPPPPPPPPqqqqiiii0q")
+VERIFY = Struct("@PPPPPPPPPPNqqqqiiii0q")
 BLOCK_COPY = Struct("@PPPPqqqqqqqqqiii0q")
 
 EXPORTS = ["sim_op_rotary", "sim_op_latent_append", "sim_op_latent_decode", "sim_op_latent_decode_workspace",
            "sim_op_latent_prefill", "sim_op_sample", "sim_op_quantized_append", "sim_op_quantized_decode",
-           "sim_op_quantized_decode_workspace", "sim_op_verify", "sim_op_block_copy", "sim_op_faults", "sim_op_last_error"]
+           "sim_op_quantized_decode_workspace", "sim_op_verify", "sim_op_verify_workspace", "sim_op_block_copy", "sim_op_faults", "sim_op_last_error"]
 
 _LIB = None
 _WORKSPACE: dict[tuple, int] = {}  # bytes by sizes
 _QUANTIZED_WORKSPACE: dict[tuple, int] = {}
+_VERIFY_WORKSPACE: dict[tuple, int] = {}
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
@@ -75,7 +76,7 @@ def lib() -> ctypes.CDLL:
                      "verify", "block_copy"):
             f = getattr(L, "sim_op_" + name)
             f.argtypes, f.restype = [ctypes.c_char_p, ctypes.c_void_p], ctypes.c_int
-        for f in (L.sim_op_latent_decode_workspace, L.sim_op_quantized_decode_workspace):
+        for f in (L.sim_op_latent_decode_workspace, L.sim_op_quantized_decode_workspace, L.sim_op_verify_workspace):
             f.argtypes, f.restype = [ctypes.c_int32] * 4, ctypes.c_size_t
         L.sim_op_faults.argtypes, L.sim_op_faults.restype = [], ctypes.c_int
         L.sim_op_last_error.argtypes, L.sim_op_last_error.restype = [], ctypes.c_char_p
@@ -559,11 +560,24 @@ def verify(target, tokens, uniform, *, draft=None, temperature=None, drafted=Non
     _packed("count", count, (b,))
     _packed("logprob", logprob, (b, places))
     device = _place(*used, out, count, logprob)
-    rc = (_LIB or lib()).sim_op_verify(
-        VERIFY.pack(target.data_ptr(), 0 if draft is None else draft.data_ptr(), tokens.data_ptr(), uniform.data_ptr(),
-                    0 if temperature is None else temperature.data_ptr(), 0 if drafted is None else drafted.data_ptr(), out.data_ptr(),
-                    count.data_ptr(), logprob.data_ptr(), rs[0], rs[1], ds[0], ds[1], b, d, vocab, code),
-        _stream_of(device))
+    L = _LIB or lib()
+    size = (device, b, d, draft is None, vocab)
+    nbytes = _VERIFY_WORKSPACE.get(size)
+    if nbytes is None:
+        nbytes = L.sim_op_verify_workspace(b, d, 0 if draft is None else 1, vocab)
+        if not nbytes:  # the device could not be asked: not an answer to keep
+            _failed(mtsim.SIM_ERR_CUDA)
+        _VERIFY_WORKSPACE[size] = nbytes
+    stream = _stream_of(device)
+    work = _scratch(nbytes, stream)
+    try:
+        rc = L.sim_op_verify(
+            VERIFY.pack(target.data_ptr(), 0 if draft is None else draft.data_ptr(), tokens.data_ptr(), uniform.data_ptr(),
+                        0 if temperature is None else temperature.data_ptr(), 0 if drafted is None else drafted.data_ptr(),
+                        out.data_ptr(), count.data_ptr(), logprob.data_ptr(), work, nbytes, rs[0], rs[1], ds[0], ds[1], b, d, vocab, code),
+            stream)
+    finally:
+        _release(work)  # what the stream allocates next comes after this call's kernels
     if rc:
         _failed(rc)
     _changed((out, count, logprob))

@@ -78,7 +78,8 @@ BAD = [
     (D, dict(cache_row=560)), (D, dict(cache_block=9216 + 16)), (D, dict(out_head=516)), (D, dict(workspace=0)), (D, dict(workspace_bytes=0)),
     (D, dict(workspace=0x10010)), (D, dict(heads=1 << 30, new_tokens=4)), (D, dict(table_blocks=1 << 28)),
     (V, dict(type=-1)), (V, dict(requests=-1)), (V, dict(drafts=-1)), (V, dict(drafts=65)), (V, dict(vocab=0)), (V, dict(vocab=(1 << 20) + 1)),
-    (V, dict(target=0)), (V, dict(tokens=0)), (V, dict(uniform=0)), (V, dict(out=0)), (V, dict(count=0)), (V, dict(requests=(1 << 24) + 1)),
+    (V, dict(target=0)), (V, dict(tokens=0)), (V, dict(uniform=0)), (V, dict(out=0)), (V, dict(count=0)), (V, dict(requests=(1 << 24) + 1)), (V, dict(workspace=0)),
+    (V, dict(workspace=0x10010)), (V, dict(workspace_bytes=0)),
     (C, dict(layers=-1)), (C, dict(rows=-1)), (C, dict(pairs=-1)), (C, dict(row_bytes=-4)), (C, dict(source_blocks=-1)),
     (C, dict(source=0)), (C, dict(destination=0)), (C, dict(from_blocks=0)), (C, dict(to_blocks=0)), (C, dict(destination_row=570)),
 ]
