@@ -1,6 +1,6 @@
 // verify.cu -- which drafted tokens the target's probabilities keep, and the
 // token that follows them (mtsim_ops.h).
-#include "ops.cuh"
+#include "tensor.cuh"
 
 #include <cooperative_groups.h>
 
@@ -11,53 +11,58 @@ namespace cg = cooperative_groups;
 
 // Two kernels.  k_rows takes all rows of logits in chunks, a block a chunk, and leaves the chunk's largest logit
 // and the sum of its weights.  k_draw, a cluster of blocks a request, joins these, decides how many tokens are
-// accepted, goes once more over the one row (or the two) that the next token is drawn from (in L2 by then), and the
+// accepted, goes once more over the one row (or the two) that the next token is drawn from, and the
 // warp whose stretch holds the point looks for it.
 // Bound by memory, the row that is drawn from by instructions: MEASURED.
 //
-// Sums of a thread's and a warp's weights are in 32 bits, beyond that in 64 (which run at a
-// sixtieth of the rate here): errors of single sums are independent, and those of 128 warps and more average out.
+// Nothing is in 64-bit floating point, which runs at a sixtieth of the rate here (a division by every thread took
+// 58 of 165 us).  Sums of single threads and warps are 32-bit floats, whose errors are independent and average out; sums
+// of those are pairs of floats, and the masses that the draw goes by are whole numbers of 2^-50, which add up the same in any order.
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBatch = 4;            // vectors that a thread has on their way
 constexpr int kMostCluster = 8;
+typedef unsigned long long u64;
 
 // log2(e) / t in two floats: (l - m) * (hi + lo) is the binary logarithm of a weight.  (Not zero for an infinite t:
 // -infinity times it is -infinity.)
 struct Rate {
     float hi, lo;
     bool greedy;
-    __device__ explicit Rate(float t) {
+    // (In 32 bits: a 64-bit division by every thread took 58 us of 64 requests' 90.)
+    __device__ __forceinline__ explicit Rate(float t) {
         greedy = !(t > 0.f);
-        const double r = greedy ? 0.0 : 1.4426950408889634 / (double)t;
-        hi = fmaxf((float)r, 1e-36f), lo = hi < INFINITY && hi > 1e-36f ? (float)(r - (double)hi) : 0.f;
-        hi = fminf(hi, 3e38f);
+        const float q = 1.44269502f / (greedy ? 1.f : t), rest = fmaf(-q, t, 1.44269502f) + 1.92596303e-8f, more = rest / t;
+        hi = fminf(fmaxf(q, 1e-36f), 3e38f), lo = hi == q && fabsf(more) < q * 1e-6f ? more : 0.f;
     }
 };
 
-__device__ __forceinline__ float exp2_near(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// A chunk, or a whole row: its largest logit, the sum of the weights 2^(rate (l - top)), and the lowest index of
-// the largest (greedy requests: all of the weight).
+// A chunk, or a whole row: its largest logit, the sum (and what it was rounded by) of the weights 2^(rate (l - top)), and
+// the lowest index of the largest (greedy requests: all of the weight).
 struct Stat {
-    double sum;
-    float top;
+    float top, sum, rest;
     int first;
+    __device__ __forceinline__ void add(float x) {
+        const float s = __fadd_rn(sum, x), b = __fsub_rn(s, sum);
+        rest += __fadd_rn(__fsub_rn(sum, __fsub_rn(s, b)), __fsub_rn(x, b));
+        sum = s;
+    }
 };
 
 // A weight to about 2^-22 of itself: the exponent's rounding (2^-24 of up to
 // 126) is kept apart and multiplied in.
-__device__ __forceinline__ float weight_of(float l, int v, float top, int first, const Rate &c) {
+template <typename T> __device__ __forceinline__ float weight_of(float l, int v, float top, int first, const Rate &c) {
     if (c.greedy) return v == first ? 1.f : 0.f;
     if (!(l > -INFINITY)) return 0.f;  // (or NaN)
     if (top == INFINITY) return l == INFINITY ? 1.f : 0.f;
-    const float d = __fsub_rn(l, top), b = __fsub_rn(d, l), off = __fsub_rn(__fsub_rn(l, __fsub_rn(d, b)), __fadd_rn(top, b));  // d + off = l - top
+    const float d = __fsub_rn(l, top);
+    float off = 0.f;  // d + off = l - top (16-bit numbers: d is exact, or so far below 0 that it does not matter)
+    if (sizeof(T) == 4) {
+        const float b = __fsub_rn(d, l);
+        off = __fsub_rn(__fsub_rn(l, __fsub_rn(d, b)), __fadd_rn(top, b));
+    }
     const float y = __fmul_rn(d, c.hi);
     if (!(y > -126.f)) return 0.f;
-    const float e = fmaf(d, c.hi, -y) + fmaf(d, c.lo, off * c.hi), p = exp2_near(y);
+    const float e = fmaf(d, c.hi, -y) + fmaf(d, c.lo, off * c.hi), p = exp2_fast(y);
     return fmaf(p, e * 0.6931471805599453f, p);
 }
 
@@ -68,52 +73,19 @@ __device__ __forceinline__ float warp_max(float v) {
 }
 __device__ __forceinline__ int warp_min(int v) { return __reduce_min_sync(~0u, v); }
 
-// Logits v .. v + N - 1 of a row that begins anywhere (v < vocab), as they lie in one or two vectors of 16 bytes;
-// results must not depend on where a row begins, so its vectors count from its first logit.
-struct Raw {
-    uint4 lo, hi;
-};
-template <typename T> __device__ __forceinline__ Raw fetch(const T *row, int v, int vocab) {
-    const uintptr_t at = (uintptr_t)(row + v);
-    const int shift = (int)(at & 15);
-    const uint4 *from = (const uint4 *)(at - shift);
-    Raw r;
-    r.lo = from[0];
-    // (the second holds an element of the row, or is not looked at)
-    if (shift && v + (16 - shift) / (int)sizeof(T) < vocab) r.hi = from[1];
-    return r;
-}
-// The same as 32-bit numbers, NaN and what lies past the row's end as -infinity.
-template <typename T> __device__ __forceinline__ void logits_of(const Raw &r, const T *row, int v, int vocab, float *f) {
+// ------------------------------------------------------------- rows -------
+// The 16 bytes at position p of a row whose first logit is `skip` elements after a 16-byte boundary, from which positions
+// count (p < vocab + skip: one of them is the row's), as 32-bit numbers; what is not the row's as -infinity.
+template <typename T> __device__ __forceinline__ void logits_of(const Vec<T> &x, int p, int skip, int vocab, float *f) {
     constexpr int N = Vec<T>::N;
-    const int shift = (int)((uintptr_t)(row + v) & 15);
-    Vec<T> x;
-    uint4 y = r.lo;
-    if (shift) {
-        uint32_t w[8] = {r.lo.x, r.lo.y, r.lo.z, r.lo.w, r.hi.x, r.hi.y, r.hi.z, r.hi.w};
-        if (shift & 8) {
-#pragma unroll
-            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-        }
-        if (shift & 4) {
-#pragma unroll
-            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-        }
-        const uint32_t by = shift & 2 ? 0x5432 : 0x3210;
-        y = make_uint4(__byte_perm(w[0], w[1], by), __byte_perm(w[1], w[2], by), __byte_perm(w[2], w[3], by), __byte_perm(w[3], w[4], by));
-    }
-    *(uint4 *)&x = y;
     x.to(f);
-#pragma unroll
-    for (int e = 0; e < N; ++e) f[e] = fmaxf(f[e], -INFINITY);
-    if (v + N > vocab) {
+    if (p < skip || p + N > vocab + skip) {
 #pragma unroll
         for (int e = 0; e < N; ++e)
-            if (v + e >= vocab) f[e] = -INFINITY;
+            if (p + e < skip || p + e >= vocab + skip) f[e] = -INFINITY;
     }
 }
 
-// ------------------------------------------------------------- rows -------
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ sim_op_verify_t a, Stat *stats, int rows, int chunks, int chunk_len) {
     constexpr int N = Vec<T>::N;
@@ -128,20 +100,21 @@ __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ si
     const T *from = k <= a.drafts ? (const T *)a.target + b * a.target_request + k * a.target_row
                                   : (const T *)a.draft + b * a.draft_request + (k - a.drafts - 1) * a.draft_row;
     const Rate c(a.temperature ? a.temperature[b] : 1.f);
-    const int begin = chunk * chunk_len, end = min(begin + chunk_len, a.vocab);
+    const int skip = (int)(((uintptr_t)from & 15) / sizeof(T)), begin = chunk * chunk_len, end = min(begin + chunk_len, a.vocab + skip);
+    const Vec<T> *x = (const Vec<T> *)(from - skip);
     float top = -INFINITY, sum = 0.f;
     int first = 0x7FFFFFFF;
     for (int p0 = begin + threadIdx.x * N; p0 < end; p0 += kBatch * kThreads * N) {
-        Raw v[kBatch];
+        Vec<T> v[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i)
-            if (p0 + i * kThreads * N < end) v[i] = fetch(from, p0 + i * kThreads * N, a.vocab);
+            if (p0 + i * kThreads * N < end) v[i] = x[p0 / N + i * kThreads];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const int p = p0 + i * kThreads * N;
             if (p >= end) break;
             float f[N];
-            logits_of(v[i], from, p, a.vocab, f);
+            logits_of(v[i], p, skip, a.vocab, f);
             float most = f[0];
 #pragma unroll
             for (int e = 1; e < N; ++e) most = fmaxf(most, f[e]);
@@ -150,12 +123,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ si
                     top = most;
 #pragma unroll
                     for (int e = N - 1; e >= 0; --e)
-                        if (f[e] == most) first = p + e;
+                        if (f[e] == most) first = p + e - skip;
                 }
                 continue;
             }
             if (most > top) {
-                sum *= exp2_near((top - most) * c.hi);
+                sum *= exp2_fast((top - most) * c.hi);
                 top = most;
                 if (top == INFINITY) sum = 0.f;  // from here on only such count
             }
@@ -163,18 +136,23 @@ __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ si
 #pragma unroll
                 for (int e = 0; e < N; ++e) sum += f[e] == INFINITY;
             } else if (top > -INFINITY) {
-                float part = 0.f;
+                float p0 = 0.f, p1 = 0.f;
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float d = f[e] - top;
-                    part += exp2_near(fmaxf(fmaf(d, c.lo, d * c.hi), -200.f));  // (-infinity times lo may be anything)
+                for (int e = 0; e < N; e += 2) {
+                    float d0 = f[e], d1 = f[e + 1], y0, y1;
+                    add2(d0, d1, -top, -top);
+                    mul2(y0, y1, d0, d1, c.hi, c.hi);
+                    fma2(y0, y1, d0, d1, c.lo, c.lo, y0, y1);
+                    // (of -infinity or NaN: NaN, and so nothing)
+                    y0 = exp2_fast(fmaxf(y0, -200.f)), y1 = exp2_fast(fmaxf(y1, -200.f));
+                    add2(p0, p1, y0, y1);
                 }
-                sum += part;
+                sum += p0 + p1;
             }
         }
     }
     const float high = warp_max(top);
-    float s = top == -INFINITY ? 0.f : high == INFINITY ? (top == INFINITY ? sum : 0.f) : sum * exp2_near((top - high) * c.hi);
+    float s = top == -INFINITY ? 0.f : high == INFINITY ? (top == INFINITY ? sum : 0.f) : sum * exp2_fast((top - high) * c.hi);
     s = warp_sum(s);
     first = warp_min(top == high ? first : 0x7FFFFFFF);
     if (lane == 0) tops[warp] = high, sums[warp] = s, firsts[warp] = first;
@@ -182,26 +160,79 @@ __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ si
     if (warp == 0) {
         const float t = lane < kWarps ? tops[lane] : -INFINITY, all = warp_max(t);
         const int f = warp_min(lane < kWarps && t == all ? firsts[lane] : 0x7FFFFFFF);
-        double w = lane < kWarps && t > -INFINITY ? (t == all ? (double)sums[lane] : (double)(sums[lane] * exp2_near((t - all) * c.hi))) : 0.0;
+        Stat r = {all, lane < kWarps && t > -INFINITY ? (t == all ? sums[lane] : sums[lane] * exp2_fast((t - all) * c.hi)) : 0.f, 0.f, f};
 #pragma unroll
-        for (int o = kWarps / 2; o; o >>= 1) w += __shfl_xor_sync(~0u, w, o);
-        if (lane == 0) stats[row * chunks + chunk] = {w, all, f};
+        for (int o = kWarps / 2; o; o >>= 1) {
+            const float s2 = __shfl_xor_sync(~0u, r.sum, o), r2 = __shfl_xor_sync(~0u, r.rest, o);
+            r.add(s2), r.rest += r2;
+        }
+        if (lane == 0) stats[row * chunks + chunk] = r;
     }
 }
 
 // ------------------------------------------------------------- draw -------
-struct Peers {
-    float mass[kWarps];  // of the block's warps' stretches
-};
+// Logits v .. v + N - 1 of a row that begins anywhere (v < vocab, the first may lie before the row), as they lie in one or two vectors of 16 bytes.
+template <typename T> __device__ __forceinline__ void logits_at(const T *row, int v, int vocab, float *f) {
+    constexpr int N = Vec<T>::N;
+    const uintptr_t at = (uintptr_t)(row + v);
+    const int shift = (int)(at & 15);
+    const uint4 *from = (const uint4 *)(at - shift);
+    Vec<T> x;
+    uint4 y = v + (16 - shift) / (int)sizeof(T) > 0 ? from[0] : make_uint4(0, 0, 0, 0);  // (each is read where it holds an element of the row)
+    if (shift) {
+        const uint4 hi = v + (16 - shift) / (int)sizeof(T) < vocab ? from[1] : make_uint4(0, 0, 0, 0);
+        uint32_t w[8] = {y.x, y.y, y.z, y.w, hi.x, hi.y, hi.z, hi.w};
+        if (shift & 8) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+        }
+        if (shift & 4) {
+#pragma unroll
+            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+        }
+        const uint32_t by = shift & 2 ? 0x5432 : 0x3210;
+        y = make_uint4(__byte_perm(w[0], w[1], by), __byte_perm(w[1], w[2], by), __byte_perm(w[2], w[3], by), __byte_perm(w[3], w[4], by));
+    }
+    *(uint4 *)&x = y;
+    x.to(f);
+    if (v < 0 || v + N > vocab) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (v + e < 0 || v + e >= vocab) f[e] = -INFINITY;
+    }
+}
+
+// A weight that is at most 1 in whole numbers of 2^-50.
+__device__ __forceinline__ u64 units_of(float w) { return __float2ull_rz(w * 0x1p50f); }
+// floor(x * f) for 0 <= f < 1 (else 0 or x) and x below 2^63.
+__device__ __forceinline__ u64 share_of(u64 x, float f) {
+    if (!(f > 0.f)) return 0;
+    if (f >= 1.f) return x;
+    const uint32_t b = __float_as_uint(f), e = b >> 23, m = (b & 0x7FFFFF) | (e ? 0x800000 : 0);
+    const int shift = 150 - (e ? e : 1);  // f = m / 2^shift, shift >= 24
+    const u64 lo = x * m, hi = __umul64hi(x, m);
+    return shift < 64 ? hi << (64 - shift) | lo >> shift : shift < 128 ? hi >> (shift - 64) : 0;
+}
+__device__ __forceinline__ u64 warp_total(u64 v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    return v;
+}
+__device__ __forceinline__ u64 warp_up_to(u64 v) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const u64 u = __shfl_up_sync(~0u, v, o);
+        if ((threadIdx.x & 31) >= o) v += u;
+    }
+    return v;
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ sim_op_verify_t a, const Stat *stats, int rows, int chunks, int stretch) {
-    constexpr int N = Vec<T>::N;
+    constexpr int N = Vec<T>::N, kParts = kMostCluster * kWarps;
     __shared__ Stat row_stat[2 * SIM_OP_MAX_DRAFTS + 1];
-    __shared__ float log_of[SIM_OP_MAX_DRAFTS + 1];
     __shared__ bool passed[SIM_OP_MAX_DRAFTS];
-    __shared__ Peers mine[2];
-    __shared__ double ahead_of[kMostCluster * kWarps], whole;
+    __shared__ u64 mass[2][kWarps], ahead_of[kParts], whole;  // mass: of the block's warps' stretches
     __shared__ int found;
     cg::cluster_group cluster = cg::this_cluster();
     const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -218,120 +249,110 @@ __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ si
     for (int k = threadIdx.x; k < rows; k += kThreads) {
         if (k <= a.drafts ? k > drafted : k - a.drafts - 1 >= drafted) continue;
         const Stat *s = stats + (b * rows + k) * chunks;
-        Stat r = {0.0, -INFINITY, 0x7FFFFFFF};
+        Stat r = {-INFINITY, 0.f, 0.f, 0x7FFFFFFF};
+        for (int i = 0; i < chunks; ++i)
+            if (s[i].top > r.top) r.top = s[i].top, r.first = s[i].first;
         for (int i = 0; i < chunks; ++i) {
             const Stat x = s[i];
-            if (x.top > r.top) r.top = x.top, r.first = x.first;
+            if (x.top == r.top) r.add(x.sum), r.rest += x.rest;
+            else if (x.top > -INFINITY && r.top < INFINITY) r.add((x.sum + x.rest) * exp2_fast((x.top - r.top) * c.hi));
         }
-        for (int i = 0; i < chunks; ++i) {
-            const Stat x = s[i];
-            if (x.top > -INFINITY) r.sum += x.top == r.top ? x.sum : r.top == INFINITY ? 0.0 : x.sum * (double)exp2_near((x.top - r.top) * c.hi);
-        }
-        if (c.greedy) r.sum = r.top > -INFINITY ? 1.0 : 0.0;
+        r.sum = c.greedy ? (float)(r.top > -INFINITY) : r.top > -INFINITY ? r.sum + r.rest : 0.f;
         row_stat[k] = r;
     }
     __syncthreads();
+    auto chance = [&](float l, int v, const Stat &p) { return p.sum > 0.f ? weight_of<T>(l, v, p.top, p.first, c) / p.sum : 0.f; };
     auto log_p = [&](float l, int v, const Stat &p) {
-        const float w = weight_of(l, v, p.top, p.first, c);
-        if (!(w > 0.f)) return -INFINITY;
+        if (!(weight_of<T>(l, v, p.top, p.first, c) > 0.f)) return -INFINITY;
         if (c.greedy) return 0.f;
-        return (float)(p.top == INFINITY ? -log(p.sum) : ((double)l - p.top) * ((double)c.hi + c.lo) * 0.6931471805599453 - log(p.sum));
+        const float d = l - p.top;
+        return (p.top == INFINITY ? 0.f : fmaf(d, c.hi, d * c.lo) * 0.6931471805599453f) - logf(p.sum);
     };
     // every drafted token's test, a token a thread
     if (threadIdx.x < drafted) {
         const int i = threadIdx.x;
         const int64_t x = tokens[i];
         const bool real = x >= 0 && x < a.vocab;
-        const Stat p = row_stat[i];
-        const float l = real ? elem<T>::to(target[i * a.target_row + x]) : -INFINITY;
-        const double px = real && p.sum > 0.0 ? weight_of(l, (int)x, p.top, p.first, c) / p.sum : 0.0;
-        double qx = real ? 1.0 : 0.0;
-        if (draft && real) {
-            const Stat q = row_stat[a.drafts + 1 + i];
-            qx = q.sum > 0.0 ? weight_of(elem<T>::to(draft[i * a.draft_row + x]), (int)x, q.top, q.first, c) / q.sum : 0.0;
-        }
+        const float px = real ? chance(elem<T>::to(target[i * a.target_row + x]), (int)x, row_stat[i]) : 0.f;
+        const float qx = !real ? 0.f : draft ? chance(elem<T>::to(draft[i * a.draft_row + x]), (int)x, row_stat[a.drafts + 1 + i]) : 1.f;
         passed[i] = uniform[i] * qx < px;
-        log_of[i] = passed[i] ? log_p(l, (int)x, p) : -INFINITY;
     }
     __syncthreads();
     int at = 0;
     while (at < drafted && passed[at]) ++at;
     // the row that is drawn from, a stretch a warp
     bool refused = at < drafted;
-    const Stat p = row_stat[at], q = refused && draft ? row_stat[a.drafts + 1 + at] : Stat{1.0, 0.f, 0};
+    const Stat p = row_stat[at], q = refused && draft ? row_stat[a.drafts + 1 + at] : Stat{0.f, 0.f, 0.f, 0};
     const T *lp = target + at * a.target_row, *lq = refused && draft ? draft + at * a.draft_row : nullptr;
     const int64_t x = refused ? tokens[at] : -1;
-    const float by_p = p.sum > 0.0 ? (float)(1.0 / p.sum) : 0.f, by_q = q.sum > 0.0 ? (float)(1.0 / q.sum) : 0.f;
-    auto weights = [&](int v, float *w) {
-        logits_of(fetch(lp, v, a.vocab), lp, v, a.vocab, w);
+    const float by_p = p.sum > 0.f ? 1.f / p.sum : 0.f, by_q = q.sum > 0.f ? 1.f / q.sum : 0.f;
+    const int skip = (int)(((uintptr_t)lp & 15) / sizeof(T)), end_at = a.vocab + skip;  // positions count from a boundary
+    auto weights = [&](int pos, float *w) {
+        const int v = pos - skip;
+        logits_of(*(const Vec<T> *)(lp + v), pos, skip, a.vocab, w);
 #pragma unroll
-        for (int e = 0; e < N; ++e) w[e] = __fmul_rn(weight_of(w[e], v + e, p.top, p.first, c), by_p);
+        for (int e = 0; e < N; ++e) w[e] = __fmul_rn(weight_of<T>(w[e], v + e, p.top, p.first, c), by_p);
         if (!refused) return;
         if (lq) {
             float g[N];
-            logits_of(fetch(lq, v, a.vocab), lq, v, a.vocab, g);
+            logits_at(lq, v, a.vocab, g);
             // (two roundings and not one fused step: equal probabilities leave nothing)
 #pragma unroll
-            for (int e = 0; e < N; ++e) w[e] = fmaxf(__fsub_rn(w[e], __fmul_rn(weight_of(g[e], v + e, q.top, q.first, c), by_q)), 0.f);
+            for (int e = 0; e < N; ++e) w[e] = fmaxf(__fsub_rn(w[e], __fmul_rn(weight_of<T>(g[e], v + e, q.top, q.first, c), by_q)), 0.f);
         } else {
 #pragma unroll
             for (int e = 0; e < N; ++e)
                 if (v + e == x) w[e] = fmaxf(__fsub_rn(w[e], 1.f), 0.f);
         }
     };
-    const int part = rank * kWarps + warp, begin = part * stretch, end = min(begin + stretch, a.vocab);
-    int chosen = -1;  // the part with the point
-    double want = 0.0;
-    for (int round = 0; round < 2; ++round) {
-        float sum = 0.f;
-        for (int v = begin + lane * N; v < end; v += 32 * N) {
-            float w[N], s = 0.f;
-            weights(v, w);
+    auto units = [&](const float *w) {
+        float s = w[0];
 #pragma unroll
-            for (int e = 0; e < N; ++e) s += w[e];
-            sum += s;
+        for (int e = 1; e < N; ++e) s += w[e];
+        return units_of(s);
+    };
+    const int part = rank * kWarps + warp, begin = part * stretch, end = min(begin + stretch, end_at);
+    int chosen = -1;  // the part with the point
+    u64 want = 0;
+    for (int round = 0; round < 2; ++round) {
+        u64 sum = 0;
+        for (int pos = begin + lane * N; pos < end; pos += 32 * N) {
+            float w[N];
+            weights(pos, w);
+            sum += units(w);
         }
-        sum = warp_sum(sum);
-        if (lane == 0) mine[round].mass[warp] = sum;
-        if (threadIdx.x == 0) found = -1;
+        sum = warp_total(sum);
+        if (lane == 0) mass[round][warp] = sum;
         if (blocks > 1) cluster.sync();
         else __syncthreads();
         const int parts = blocks * kWarps;
         if (warp == 0) {
             // the masses ahead of every part, four parts a lane
-            double before = 0.0, m[kMostCluster * kWarps / 32];
+            u64 m[kParts / 32], all = 0;
 #pragma unroll
-            for (int k = 0; k < kMostCluster * kWarps / 32; ++k) {
-                const int i = lane * (kMostCluster * kWarps / 32) + k;
-                m[k] = i < parts ? (double)(blocks > 1 ? cluster.map_shared_rank(&mine[round], i / kWarps) : &mine[round])->mass[i % kWarps] : 0.0;
-                before += m[k];
+            for (int k = 0; k < kParts / 32; ++k) {
+                const int i = lane * (kParts / 32) + k;
+                m[k] = i >= parts ? 0 : blocks > 1 ? cluster.map_shared_rank(&mass[round][0], i / kWarps)[i % kWarps] : mass[round][i];
+                all += m[k];
             }
-            double incl = before;
+            const u64 up_to = warp_up_to(all), total = __shfl_sync(~0u, up_to, 31), point = share_of(total, uniform[a.drafts]);
+            u64 run = up_to - all;
+            int here = 0x7FFFFFFF;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double u = __shfl_up_sync(~0u, incl, o);
-                if (lane >= o) incl += u;
-            }
-            const double total = __shfl_sync(~0u, incl, 31), point = uniform[a.drafts] * total;
-            double run = incl - before;
-            int here = 0x7FFFFFFF, last = -1;
-#pragma unroll
-            for (int k = 0; k < kMostCluster * kWarps / 32; ++k) {
-                const int i = lane * (kMostCluster * kWarps / 32) + k;
+            for (int k = 0; k < kParts / 32; ++k) {
+                const int i = lane * (kParts / 32) + k;
                 if (i < parts) ahead_of[i] = run;
                 run += m[k];
-                if (m[k] > 0.0) {
-                    last = i;
-                    if (run > point && here == 0x7FFFFFFF) here = i;
-                }
+                if (run > point && here == 0x7FFFFFFF) here = i;
             }
-            here = warp_min(here), last = __reduce_max_sync(~0u, last);
-            if (lane == 0) whole = total, found = here == 0x7FFFFFFF ? last : here;  // (rounding may leave none above)
+            here = warp_min(here);
+            if (lane == 0) whole = total, found = total ? here : -1;
         }
         __syncthreads();
-        chosen = found, want = uniform[a.drafts] * whole;
+        chosen = found, want = share_of(whole, uniform[a.drafts]);
         if (chosen >= 0 || !refused) break;
         refused = false;  // nothing is left: from p itself
+        __syncthreads();
     }
     int64_t *out = a.out + b * (a.drafts + 1);
     float *logprob = a.logprob ? a.logprob + b * (a.drafts + 1) : nullptr;
@@ -341,35 +362,29 @@ __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ si
         a.count[b] = at + 1;
     };
     if (chosen == part) {
-        double before = ahead_of[part];
-        int token = -1, last = -1;
-        for (int v0 = begin; v0 < end && token < 0; v0 += 32 * N) {
-            const int v = v0 + lane * N;
-            float w[N], s = 0.f;
-            if (v < end) weights(v, w);
+        u64 before = ahead_of[part];
+        int token = -1;
+        for (int p0 = begin; p0 < end && token < 0; p0 += 32 * N) {
+            const int pos = p0 + lane * N;
+            float w[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) s += v < end ? w[e] : 0.f;
-            double incl = s;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double u = __shfl_up_sync(~0u, incl, o);
-                if (lane >= o) incl += u;
-            }
-            const unsigned above = __ballot_sync(~0u, before + incl > want);
-            int mine_last = -1, hit = -1;
-            double run = before + incl - s;
+            for (int e = 0; e < N; ++e) w[e] = 0.f;
+            if (pos < end) weights(pos, w);
+            const u64 own = units(w), up_to = warp_up_to(own);
+            const unsigned above = __ballot_sync(~0u, before + up_to > want);
+            int hit = -1, last = -1;  // (the vector's sum was rounded: the last with weight, should none reach the point)
+            u64 run = before + up_to - own;
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                if (v < end && w[e] > 0.f) {
-                    mine_last = v + e;
-                    run += w[e];
-                    if (hit < 0 && run > want) hit = v + e;
+                if (w[e] > 0.f) {
+                    last = pos + e;
+                    run += units_of(w[e]);
+                    if (hit < 0 && run > want) hit = pos + e;
                 }
-            if (above) token = __shfl_sync(~0u, hit >= 0 ? hit : mine_last, __ffs(above) - 1);
-            last = max(last, __reduce_max_sync(~0u, mine_last));
-            before += __shfl_sync(~0u, incl, 31);
+            if (above) token = __shfl_sync(~0u, hit >= 0 ? hit : last, __ffs(above) - 1) - skip;
+            before += __shfl_sync(~0u, up_to, 31);
         }
-        if (lane == 0) drawn(token >= 0 ? token : last);
+        if (lane == 0) drawn(token);
     } else if (chosen < 0 && part == 0 && lane == 0) {
         drawn(-1);
     }
@@ -377,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ si
         for (int i = threadIdx.x; i <= a.drafts; i += kThreads)
             if (i != at) {
                 out[i] = i < at ? tokens[i] : -1;
-                if (logprob) logprob[i] = i < at ? log_of[i] : -INFINITY;
+                if (logprob) logprob[i] = i < at ? log_p(elem<T>::to(target[i * a.target_row + tokens[i]]), (int)tokens[i], row_stat[i]) : -INFINITY;
             }
     }
     if (blocks > 1) cluster.sync();  // no block leaves while another reads its masses
@@ -401,13 +416,13 @@ Cut cut_for(int sms, int64_t requests, int drafts, bool known, int vocab) {
 
 template <typename T> int run(const sim_op_verify_t *a, const Cut &c, cudaStream_t st) {
     constexpr int N = Vec<T>::N;
-    const int chunk_len = ((a->vocab + c.chunks - 1) / c.chunks + N - 1) / N * N;
+    const int chunk_len = ((a->vocab + N - 1 + c.chunks - 1) / c.chunks + N - 1) / N * N;  // positions, which begin up to N - 1 before the row
     Stat *stats = (Stat *)a->workspace;
     cudaError_t e = launch_early(k_rows<T>, (unsigned)(a->requests * (int64_t)c.rows * c.chunks), kThreads, 0, 1, st, *a, stats, c.rows, c.chunks, chunk_len);
     if (e != cudaSuccess) return launched("sim_op_verify (rows)", e);
     int blocks = 1;
     while (blocks < kMostCluster && a->vocab > blocks * 4096) blocks *= 2;
-    const int step = 32 * N, parts = blocks * kWarps, stretch = ((a->vocab + parts - 1) / parts + step - 1) / step * step;
+    const int step = 32 * N, parts = blocks * kWarps, stretch = ((a->vocab + N - 1 + parts - 1) / parts + step - 1) / step * step;
     e = launch_early(k_draw<T>, (unsigned)(a->requests * (int64_t)blocks), kThreads, 0, blocks, st, *a, (const Stat *)stats, c.rows, c.chunks, stretch);
     return launched("sim_op_verify (draw)", e);
 }
