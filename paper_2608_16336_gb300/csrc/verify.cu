@@ -36,6 +36,26 @@ struct Rate {
     }
 };
 
+// Two floats in a register pair, so that what is the same for all logits is put into one once.
+__device__ __forceinline__ u64 pair_of(float x, float y) {
+    u64 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void parts_of(u64 r, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(r)); }
+__device__ __forceinline__ u64 pair_add(u64 x, u64 y) {
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(x) : "l"(y));
+    return x;
+}
+__device__ __forceinline__ u64 pair_mul(u64 x, u64 y) {
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(x) : "l"(y));
+    return x;
+}
+__device__ __forceinline__ u64 pair_fma(u64 x, u64 y, u64 z) {
+    asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(x) : "l"(y), "l"(z));
+    return x;
+}
+
 // A chunk, or a whole row: its largest logit, the sum (and what it was rounded by) of the weights 2^(rate (l - top)), and
 // the lowest index of the largest (greedy requests: all of the weight).
 struct Stat {
@@ -104,6 +124,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ si
     const Vec<T> *x = (const Vec<T> *)(from - skip);
     float top = -INFINITY, sum = 0.f;
     int first = 0x7FFFFFFF;
+    const u64 hi = pair_of(c.hi, c.hi), lo = pair_of(c.lo, c.lo);
+    u64 less = 0;  // -top, twice
     for (int p0 = begin + threadIdx.x * N; p0 < end; p0 += kBatch * kThreads * N) {
         Vec<T> v[kBatch];
 #pragma unroll
@@ -129,24 +151,24 @@ __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ si
             }
             if (most > top) {
                 sum *= exp2_fast((top - most) * c.hi);
-                top = most;
+                top = most, less = pair_of(-top, -top);
                 if (top == INFINITY) sum = 0.f;  // from here on only such count
             }
             if (top == INFINITY) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) sum += f[e] == INFINITY;
             } else if (top > -INFINITY) {
-                float p0 = 0.f, p1 = 0.f;
+                u64 part = 0;
 #pragma unroll
                 for (int e = 0; e < N; e += 2) {
-                    float d0 = f[e], d1 = f[e + 1], y0, y1;
-                    add2(d0, d1, -top, -top);
-                    mul2(y0, y1, d0, d1, c.hi, c.hi);
-                    fma2(y0, y1, d0, d1, c.lo, c.lo, y0, y1);
+                    const u64 d = pair_add(pair_of(f[e], f[e + 1]), less);
+                    float y0, y1;
+                    parts_of(pair_fma(d, lo, pair_mul(d, hi)), y0, y1);
                     // (of -infinity or NaN: NaN, and so nothing)
-                    y0 = exp2_fast(fmaxf(y0, -200.f)), y1 = exp2_fast(fmaxf(y1, -200.f));
-                    add2(p0, p1, y0, y1);
+                    part = pair_add(part, pair_of(exp2_fast(fmaxf(y0, -200.f)), exp2_fast(fmaxf(y1, -200.f))));
                 }
+                float p0, p1;
+                parts_of(part, p0, p1);
                 sum += p0 + p1;
             }
         }
@@ -229,10 +251,11 @@ __device__ __forceinline__ u64 warp_up_to(u64 v) {
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ sim_op_verify_t a, const Stat *stats, int rows, int chunks, int stretch) {
-    constexpr int N = Vec<T>::N, kParts = kMostCluster * kWarps;
+    constexpr int N = Vec<T>::N, kParts = kMostCluster * kWarps, kSteps = 16;  // steps whose masses are kept
     __shared__ Stat row_stat[2 * SIM_OP_MAX_DRAFTS + 1];
     __shared__ bool passed[SIM_OP_MAX_DRAFTS];
     __shared__ u64 mass[2][kWarps], ahead_of[kParts], whole;  // mass: of the block's warps' stretches
+    __shared__ u64 step_mass[kWarps][kSteps];
     __shared__ int found;
     cg::cluster_group cluster = cg::this_cluster();
     const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -245,20 +268,30 @@ __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ si
     const T *target = (const T *)a.target + b * a.target_request, *draft = a.draft ? (const T *)a.draft + b * a.draft_request : nullptr;
     const int64_t *tokens = a.tokens + b * a.drafts;
     const float *uniform = a.uniform + b * (a.drafts + 1);
-    // the rows' chunks, a row a thread
-    for (int k = threadIdx.x; k < rows; k += kThreads) {
+    // the rows' chunks, a row a warp
+    for (int k = warp; k < rows; k += kWarps) {
         if (k <= a.drafts ? k > drafted : k - a.drafts - 1 >= drafted) continue;
         const Stat *s = stats + (b * rows + k) * chunks;
         Stat r = {-INFINITY, 0.f, 0.f, 0x7FFFFFFF};
-        for (int i = 0; i < chunks; ++i)
-            if (s[i].top > r.top) r.top = s[i].top, r.first = s[i].first;
-        for (int i = 0; i < chunks; ++i) {
-            const Stat x = s[i];
-            if (x.top == r.top) r.add(x.sum), r.rest += x.rest;
-            else if (x.top > -INFINITY && r.top < INFINITY) r.add((x.sum + x.rest) * exp2_fast((x.top - r.top) * c.hi));
+        for (int i0 = 0; i0 < chunks; i0 += 32) {  // (one round for up to 32 chunks)
+            const Stat x = i0 + lane < chunks ? s[i0 + lane] : Stat{-INFINITY, 0.f, 0.f, 0x7FFFFFFF};
+            const float top = fmaxf(r.top, warp_max(x.top));
+            const int first = warp_min(x.top == top ? x.first : 0x7FFFFFFF);
+            const float by = r.top == top ? 1.f : r.top > -INFINITY && top < INFINITY ? exp2_fast((r.top - top) * c.hi) : 0.f;
+            r.sum *= by, r.rest *= by;
+            if (top > r.top) r.first = first;
+            r.top = top;
+            const float own = x.top == top ? 1.f : x.top > -INFINITY && top < INFINITY ? exp2_fast((x.top - top) * c.hi) : 0.f;
+            Stat t = {top, x.sum * own, x.rest * own, 0};
+#pragma unroll
+            for (int o = 16; o; o >>= 1) {
+                const float s2 = __shfl_xor_sync(~0u, t.sum, o), r2 = __shfl_xor_sync(~0u, t.rest, o);
+                t.add(s2), t.rest += r2;
+            }
+            r.add(t.sum), r.rest += t.rest;
         }
         r.sum = c.greedy ? (float)(r.top > -INFINITY) : r.top > -INFINITY ? r.sum + r.rest : 0.f;
-        row_stat[k] = r;
+        if (lane == 0) row_stat[k] = r;
     }
     __syncthreads();
     auto chance = [&](float l, int v, const Stat &p) { return p.sum > 0.f ? weight_of<T>(l, v, p.top, p.first, c) / p.sum : 0.f; };
@@ -316,10 +349,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ si
     u64 want = 0;
     for (int round = 0; round < 2; ++round) {
         u64 sum = 0;
-        for (int pos = begin + lane * N; pos < end; pos += 32 * N) {
+        for (int p0 = begin, k = 0; p0 < end; p0 += 32 * N, ++k) {
+            const int pos = p0 + lane * N;
             float w[N];
-            weights(pos, w);
-            sum += units(w);
+            u64 own = 0;
+            if (pos < end) weights(pos, w), own = units(w);
+            if (k < kSteps) {
+                own = warp_total(own);
+                if (lane == 0) step_mass[warp][k] = own;
+                sum += lane == 0 ? own : 0;
+            } else {
+                sum += own;
+            }
         }
         sum = warp_total(sum);
         if (lane == 0) mass[round][warp] = sum;
@@ -363,8 +404,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ si
     };
     if (chosen == part) {
         u64 before = ahead_of[part];
-        int token = -1;
-        for (int p0 = begin; p0 < end && token < 0; p0 += 32 * N) {
+        int token = -1, p0 = begin;
+        for (int k = 0; k < kSteps && p0 < end && before + step_mass[warp][k] <= want; ++k) before += step_mass[warp][k], p0 += 32 * N;
+        for (; p0 < end && token < 0; p0 += 32 * N) {
             const int pos = p0 + lane * N;
             float w[N];
 #pragma unroll
@@ -414,14 +456,15 @@ Cut cut_for(int sms, int64_t requests, int drafts, bool known, int vocab) {
     return c;
 }
 
-template <typename T> int run(const sim_op_verify_t *a, const Cut &c, cudaStream_t st) {
+template <typename T> int run(const sim_op_verify_t *a, const Cut &c, int sms, cudaStream_t st) {
     constexpr int N = Vec<T>::N;
     const int chunk_len = ((a->vocab + N - 1 + c.chunks - 1) / c.chunks + N - 1) / N * N;  // positions, which begin up to N - 1 before the row
     Stat *stats = (Stat *)a->workspace;
     cudaError_t e = launch_early(k_rows<T>, (unsigned)(a->requests * (int64_t)c.rows * c.chunks), kThreads, 0, 1, st, *a, stats, c.rows, c.chunks, chunk_len);
     if (e != cudaSuccess) return launched("sim_op_verify (rows)", e);
+    // as many blocks as run at once, of 4,096 logits at least
     int blocks = 1;
-    while (blocks < kMostCluster && a->vocab > blocks * 4096) blocks *= 2;
+    while (blocks < kMostCluster && a->vocab > blocks * 4096 && 2 * blocks * (int64_t)a->requests <= 2 * sms) blocks *= 2;
     const int step = 32 * N, parts = blocks * kWarps, stretch = ((a->vocab + N - 1 + parts - 1) / parts + step - 1) / step * step;
     e = launch_early(k_draw<T>, (unsigned)(a->requests * (int64_t)blocks), kThreads, 0, blocks, st, *a, (const Stat *)stats, c.rows, c.chunks, stretch);
     return launched("sim_op_verify (draw)", e);
@@ -459,6 +502,6 @@ extern "C" int sim_op_verify(const sim_op_verify_t *a, void *stream) {
         return fail(SIM_ERR_ARG, "requests * rows is too large");
     if (a->workspace_bytes < c.bytes) return fail(SIM_ERR_ARG, "the workspace must have %zu bytes", c.bytes);
     const cudaStream_t st = (cudaStream_t)stream;
-    if (a->type == SIM_OP_BF16) return run<__nv_bfloat16>(a, c, st);
-    return a->type == SIM_OP_FP16 ? run<__half>(a, c, st) : run<float>(a, c, st);
+    if (a->type == SIM_OP_BF16) return run<__nv_bfloat16>(a, c, sms, st);
+    return a->type == SIM_OP_FP16 ? run<__half>(a, c, sms, st) : run<float>(a, c, sms, st);
 }
