@@ -86,6 +86,26 @@ template <typename T> __device__ __forceinline__ float weight_of(float l, int v,
     return fmaf(p, e * 0.6931471805599453f, p);
 }
 
+// The weights of a vector's logits, to the same accuracy, where the row's largest is a number.
+template <typename T, int N> __device__ __forceinline__ void weights_of(float *l, int v, float top, int first, const Rate &c) {
+    if (c.greedy || !(fabsf(top) < INFINITY) || sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) l[e] = weight_of<T>(l[e], v + e, top, first, c);
+        return;
+    }
+    const u64 less = pair_of(-top, -top), hi = pair_of(c.hi, c.hi), lo = pair_of(c.lo, c.lo), minus = pair_of(-1.f, -1.f),
+              ln2 = pair_of(0.6931471805599453f, 0.6931471805599453f);
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+        const u64 d = pair_add(pair_of(l[e], l[e + 1]), less), y = pair_mul(d, hi), off = pair_fma(d, lo, pair_fma(d, hi, pair_mul(y, minus)));
+        float y0, y1;
+        parts_of(y, y0, y1);
+        const u64 p = pair_of(exp2_fast(y0), exp2_fast(y1));
+        parts_of(pair_fma(p, pair_mul(off, ln2), p), l[e], l[e + 1]);
+        l[e] = y0 > -126.f ? l[e] : 0.f, l[e + 1] = y1 > -126.f ? l[e + 1] : 0.f;
+    }
+}
+
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
@@ -113,8 +133,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ si
     __shared__ int firsts[kWarps];
     let_next_start();
     after_previous();
-    const int64_t row = blockIdx.x / chunks, b = row / rows;
-    const int chunk = (int)(blockIdx.x - row * chunks), k = (int)(row - b * rows), lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const uint32_t row = blockIdx.x / (uint32_t)chunks, in = row / (uint32_t)rows;
+    const int64_t b = in;
+    const int chunk = (int)(blockIdx.x - row * chunks), k = (int)(row - in * rows), lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int drafted = a.drafted ? min(max(a.drafted[b], 0), a.drafts) : a.drafts;
     if (k <= a.drafts ? k > drafted : k - a.drafts - 1 >= drafted) return;  // of a token that is not there
     const T *from = k <= a.drafts ? (const T *)a.target + b * a.target_request + k * a.target_row
@@ -188,7 +209,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ si
             const float s2 = __shfl_xor_sync(~0u, r.sum, o), r2 = __shfl_xor_sync(~0u, r.rest, o);
             r.add(s2), r.rest += r2;
         }
-        if (lane == 0) stats[row * chunks + chunk] = r;
+        if (lane == 0) stats[(int64_t)row * chunks + chunk] = r;
     }
 }
 
@@ -259,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ si
     __shared__ int found;
     cg::cluster_group cluster = cg::this_cluster();
     const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int64_t b = blockIdx.x / blocks;
+    const int64_t b = blockIdx.x / (uint32_t)blocks;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     let_next_start();
     after_previous();
@@ -323,15 +344,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ si
     auto weights = [&](int pos, float *w) {
         const int v = pos - skip;
         logits_of(*(const Vec<T> *)(lp + v), pos, skip, a.vocab, w);
+        weights_of<T, N>(w, v, p.top, p.first, c);
 #pragma unroll
-        for (int e = 0; e < N; ++e) w[e] = __fmul_rn(weight_of<T>(w[e], v + e, p.top, p.first, c), by_p);
+        for (int e = 0; e < N; ++e) w[e] = __fmul_rn(w[e], by_p);
         if (!refused) return;
         if (lq) {
             float g[N];
             logits_at(lq, v, a.vocab, g);
+            weights_of<T, N>(g, v, q.top, q.first, c);
             // (two roundings and not one fused step: equal probabilities leave nothing)
 #pragma unroll
-            for (int e = 0; e < N; ++e) w[e] = fmaxf(__fsub_rn(w[e], __fmul_rn(weight_of<T>(g[e], v + e, q.top, q.first, c), by_q)), 0.f);
+            for (int e = 0; e < N; ++e) w[e] = fmaxf(__fsub_rn(w[e], __fmul_rn(g[e], by_q)), 0.f);
         } else {
 #pragma unroll
             for (int e = 0; e < N; ++e)
@@ -440,7 +463,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ si
     if (blocks > 1) cluster.sync();  // no block leaves while another reads its masses
 }
 
-// How the rows are cut: as many chunks as give all multiprocessors some, of 2,048 to 16,384 logits and a few more.
+// How the rows are cut: as many chunks as give all multiprocessors some, of 2,048 to 65,536 logits (what a block
+// does besides is as much as 10 instructions a logit of 14,000).
 struct Cut {
     int rows, chunks;
     size_t bytes;
@@ -449,7 +473,7 @@ Cut cut_for(int sms, int64_t requests, int drafts, bool known, int vocab) {
     Cut c;
     c.rows = known ? 2 * drafts + 1 : drafts + 1;
     int64_t chunks = (4 * (int64_t)sms + requests * c.rows - 1) / (requests * c.rows);
-    const int64_t least = (vocab + 17000) / 17001, most = (vocab + 2047) / 2048;
+    const int64_t least = (vocab + 65535) / 65536, most = (vocab + 2047) / 2048;
     chunks = chunks < least ? least : chunks > most ? most : chunks;
     c.chunks = (int)chunks;
     c.bytes = sizeof(Stat) * (size_t)requests * c.rows * c.chunks;
