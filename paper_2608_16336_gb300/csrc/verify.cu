@@ -126,6 +126,43 @@ template <typename T> __device__ __forceinline__ void logits_of(const Vec<T> &x,
     }
 }
 
+// A vector of logits as they are held: the largest (NaN left out), and 32-bit pairs of those not below `low`.
+template <typename T> struct Held;
+template <> struct Held<__nv_bfloat16> {
+    static constexpr float low = -1.00000000e+30f;
+    __device__ static float largest(const uint4 &x) {
+        __nv_bfloat162 m = __hmax2(__hmax2(*(const __nv_bfloat162 *)&x.x, *(const __nv_bfloat162 *)&x.y), __hmax2(*(const __nv_bfloat162 *)&x.z, *(const __nv_bfloat162 *)&x.w));
+        const uint32_t w = *(const uint32_t *)&m;
+        return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    }
+    __device__ static u64 pair(const uint4 &x, int i) {
+        const uint32_t w = (&x.x)[i];
+        return pair_of(fmaxf(__uint_as_float(w << 16), low), fmaxf(__uint_as_float(w & 0xFFFF0000u), low));
+    }
+};
+template <> struct Held<__half> {
+    static constexpr float low = -65504.f;
+    __device__ static float largest(const uint4 &x) {
+        const __half2 m = __hmax2(__hmax2(*(const __half2 *)&x.x, *(const __half2 *)&x.y), __hmax2(*(const __half2 *)&x.z, *(const __half2 *)&x.w));
+        const float2 f = __half22float2(m);
+        return fmaxf(f.x, f.y);
+    }
+    __device__ static u64 pair(const uint4 &x, int i) {
+        const float2 f = __half22float2(*(const __half2 *)(&x.x + i));
+        return pair_of(fmaxf(f.x, low), fmaxf(f.y, low));
+    }
+};
+template <> struct Held<float> {
+    static constexpr float low = -1.00000000e+30f;
+    __device__ static float largest(const uint4 &x) {
+        return fmaxf(fmaxf(__uint_as_float(x.x), __uint_as_float(x.y)), fmaxf(__uint_as_float(x.z), __uint_as_float(x.w)));
+    }
+    __device__ static u64 pair(const uint4 &x, int i) {
+        const uint32_t *w = &x.x + 2 * i;
+        return pair_of(fmaxf(__uint_as_float(w[0]), low), fmaxf(__uint_as_float(w[1]), low));
+    }
+};
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ sim_op_verify_t a, Stat *stats, int rows, int chunks, int chunk_len) {
     constexpr int N = Vec<T>::N;
@@ -145,9 +182,52 @@ __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ si
     const Vec<T> *x = (const Vec<T> *)(from - skip);
     float top = -INFINITY, sum = 0.f;
     int first = 0x7FFFFFFF;
-    const u64 hi = pair_of(c.hi, c.hi), lo = pair_of(c.lo, c.lo);
-    u64 less = 0;  // -top, twice
-    for (int p0 = begin + threadIdx.x * N; p0 < end; p0 += kBatch * kThreads * N) {
+    // Without a branch for a logit's kind: -infinity and NaN count as the lowest number `low`, whose weight is 0 under any larger
+    // logit (a temperature within reason), and the largest is taken anew with every vector.  Threads that
+    // find nothing larger than that, or +infinity, look again below.
+    const bool plain = !c.greedy && c.hi < 1e6f && c.hi > 0.01f;
+    if (plain) {
+        const u64 hi = pair_of(c.hi, c.hi), lo = pair_of(c.lo, c.lo);
+        float high = Held<T>::low;
+        for (int p0 = begin + threadIdx.x * N; p0 < end; p0 += kBatch * kThreads * N) {
+            uint4 v[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (p0 + i * kThreads * N < end) v[i] = *(const uint4 *)(x + p0 / N + i * kThreads);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int p = p0 + i * kThreads * N;
+                if (p >= end) break;
+                if (p < skip || p + N > a.vocab + skip) {
+                    T *t = (T *)&v[i];
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (p + e < skip || p + e >= a.vocab + skip) t[e] = elem<T>::from(-INFINITY);
+                }
+                const float most = Held<T>::largest(v[i]), now = fmaxf(high, most);
+                top = fmaxf(top, most);
+                sum *= exp2_fast((high - now) * c.hi);
+                high = now;
+                const u64 less = pair_of(-now, -now);
+                u64 part = 0;
+#pragma unroll
+                for (int e = 0; e < N / 2; ++e) {
+                    const u64 d = pair_add(Held<T>::pair(v[i], e), less);
+                    float y0, y1;
+                    parts_of(pair_fma(d, lo, pair_mul(d, hi)), y0, y1);
+                    part = pair_add(part, pair_of(exp2_fast(y0), exp2_fast(y1)));
+                }
+                float s0, s1;
+                parts_of(part, s0, s1);
+                sum += s0 + s1;
+            }
+        }
+        if (top == -INFINITY) sum = 0.f;
+    }
+    // one by one
+    const bool again = plain && (top == INFINITY || (top > -INFINITY && top <= Held<T>::low));
+    if (again) top = -INFINITY, sum = 0.f;
+    if (!plain || again) for (int p0 = begin + threadIdx.x * N; p0 < end; p0 += kBatch * kThreads * N) {
         Vec<T> v[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i)
@@ -172,25 +252,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ si
             }
             if (most > top) {
                 sum *= exp2_fast((top - most) * c.hi);
-                top = most, less = pair_of(-top, -top);
+                top = most;
                 if (top == INFINITY) sum = 0.f;  // from here on only such count
             }
             if (top == INFINITY) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) sum += f[e] == INFINITY;
             } else if (top > -INFINITY) {
-                u64 part = 0;
 #pragma unroll
-                for (int e = 0; e < N; e += 2) {
-                    const u64 d = pair_add(pair_of(f[e], f[e + 1]), less);
-                    float y0, y1;
-                    parts_of(pair_fma(d, lo, pair_mul(d, hi)), y0, y1);
-                    // (of -infinity or NaN: NaN, and so nothing)
-                    part = pair_add(part, pair_of(exp2_fast(fmaxf(y0, -200.f)), exp2_fast(fmaxf(y1, -200.f))));
+                for (int e = 0; e < N; ++e) {
+                    const float d = f[e] - top;
+                    sum += exp2_fast(fmaxf(fmaf(d, c.lo, d * c.hi), -200.f));  // (of -infinity or NaN: NaN, and so nothing)
                 }
-                float p0, p1;
-                parts_of(part, p0, p1);
-                sum += p0 + p1;
             }
         }
     }
