@@ -19,6 +19,11 @@ times iterations of mixed batches, ``fit_iteration_times`` gives base, a and b, 
 
 Weights are random; the layers are attention layers with their projections
 (plain matrix products), and ``feed_forward`` adds what else a layer does.
+
+An instance's cache is of the shape's type, or (``quantized``) of 8-bit
+numbers with scales.  ``speculate`` advances the running requests by drafted
+tokens, ``fork`` lets requests share their blocks, ``migrate`` moves one to
+another instance's cache and ``compact`` the used blocks to the start.
 """
 from __future__ import annotations
 
@@ -65,10 +70,14 @@ def _norm(x):
 
 class Instance:
     """An instance with ``blocks`` cache blocks of ``block_tokens`` tokens and at
-    most ``max_batch`` running requests, on the current CUDA device."""
+    most ``max_batch`` running requests, on the current CUDA device;
+    ``quantized`` holds the cache in 8 bits (``instance_ops.quantized_append``)."""
+
+    shared: dict[int, int] = {}  # blocks that more than one request holds, by how many more; replaced, never changed in place
+    scales = None
 
     def __init__(self, shape: Shape = Shape(), *, blocks: int, block_tokens: int, max_batch: int = 64, seed: int = 0,
-                 frequencies: torch.Tensor | None = None, feed_forward=None):
+                 frequencies: torch.Tensor | None = None, feed_forward=None, quantized: bool = False):
         if blocks < 1 or block_tokens < 1 or max_batch < 1:
             raise ValueError("blocks, block_tokens and max_batch must be at least 1")
         self.shape, self.block_tokens, self.max_batch, self.feed_forward = shape, block_tokens, max_batch, feed_forward
@@ -89,6 +98,9 @@ class Instance:
                             value_up=weight(s.heads, s.rank, s.value_dim, fan=s.rank),
                             out=weight(s.heads * s.value_dim, s.hidden, fan=s.heads * s.value_dim)) for _ in range(s.layers)]
         self.cache = torch.zeros(s.layers, blocks, block_tokens, s.rank + s.key_dim, dtype=s.dtype, device="cuda")
+        if quantized:
+            self.cache = self.cache.to(ops.EIGHT)
+            self.scales = torch.ones(s.layers, blocks, 2, device="cuda")
         self.unembed = weight(s.hidden, s.vocab, fan=s.hidden)
 
     # -- the cache
@@ -108,9 +120,47 @@ class Instance:
             taken += k
         return blocks, taken
 
+    def _give_back(self, blocks) -> None:
+        """Frees blocks, those alone that no other request holds."""
+        shared = dict(self.shared)
+        for b in blocks:
+            if b not in shared:
+                self.free.append(b)
+            elif shared[b] > 1:
+                shared[b] -= 1
+            else:
+                del shared[b]
+        self.shared = shared
+
+    def _own(self, blocks, first, taken):
+        """``blocks`` with those that a request is about to write (from its
+        token ``first`` on) and others hold too replaced by free ones, how many free
+        ones are taken with these, and the pairs to be copied.  Changes nothing."""
+        copies, blocks = [], [list(b) for b in blocks]
+        left = dict(self.shared)
+        for b, n in zip(blocks, first):
+            for i in range(n // self.block_tokens, len(b)):
+                if left.get(b[i]):
+                    if taken >= len(self.free):
+                        raise RuntimeError("out of cache blocks: none is free for a block that requests share")
+                    left[b[i]] -= 1
+                    copies.append((b[i], self.free[-1 - taken]))
+                    b[i] = self.free[-1 - taken]
+                    taken += 1
+        return blocks, taken, copies
+
+    def _copy(self, pairs, other=None) -> None:
+        """Copies blocks of the cache, and their scales, to blocks of ``other``'s (default: this one's)."""
+        if pairs:
+            other = self if other is None else other
+            a, b = torch.tensor(list(zip(*pairs)), dtype=torch.int32, device="cuda")
+            ops.block_copy(self.cache, other.cache, a, b)
+            if self.scales is not None:
+                ops.block_copy(self.scales, other.scales, a, b)
+
     def release(self, request: int) -> None:
         """Takes a request out of the batch and gives its blocks back."""
-        self.free += self.running.pop(request).blocks[::-1]
+        self._give_back(self.running.pop(request).blocks[::-1])
 
     def rewind(self, request: int, tokens: int) -> None:
         """Takes a running request back to its first ``tokens`` cached tokens."""
@@ -118,8 +168,57 @@ class Instance:
         if not 1 <= tokens <= q.length:
             raise ValueError("a request of %d tokens cannot go back to %d" % (q.length, tokens))
         q.length = tokens
-        while len(q.blocks) > self.blocks_for(tokens):
-            self.free.append(q.blocks.pop())
+        keep = self.blocks_for(tokens)
+        self._give_back(q.blocks[keep:][::-1])
+        del q.blocks[keep:]
+
+    def fork(self, request: int, copies: int = 1) -> list[int]:
+        """Adds ``copies`` requests that go on from where ``request`` is, with its
+        full blocks; a block that is not full is copied.  Returns their numbers."""
+        q = self.running[request]
+        if copies < 1 or len(self.running) + copies > self.max_batch:
+            raise ValueError("more than max_batch = %d requests, or no copy" % self.max_batch)
+        part = q.length % self.block_tokens > 0
+        if part and copies > len(self.free):
+            raise RuntimeError("out of cache blocks: %d wanted, %d free" % (copies, len(self.free)))
+        own = [self.free[-1 - i] for i in range(copies)] if part else [None] * copies
+        self._copy([(q.blocks[-1], b) for b in own] if part else [])
+        if part:
+            del self.free[len(self.free) - copies:]
+        full, ids = q.blocks[:-1] if part else q.blocks, []
+        self.shared = {**self.shared, **{b: self.shared.get(b, 0) + copies for b in full}}
+        for b in own:
+            self.running[self._next] = Running(full + ([b] if part else []), q.length, q.token)
+            ids.append(self._next)
+            self._next += 1
+        return ids
+
+    def migrate(self, request: int, other: "Instance") -> int:
+        """Moves a running request into ``other``'s batch and cache; returns its number there."""
+        if other is self or self.shape != other.shape or self.block_tokens != other.block_tokens or (self.scales is None) != (other.scales is None):
+            raise ValueError("a request moves to another instance with the same shape, block size and cache type")
+        if len(other.running) >= other.max_batch:
+            raise ValueError("more than max_batch = %d requests" % other.max_batch)
+        q = self.running[request]
+        (blocks,), taken = other._plan([[]], [q.length])
+        self._copy(list(zip(q.blocks, blocks)), other)
+        del other.free[len(other.free) - taken:]
+        there, other._next = other._next, other._next + 1
+        other.running[there] = Running(blocks, q.length, q.token)
+        self.release(request)
+        return there
+
+    def compact(self) -> int:
+        """Moves the used blocks to the start of the cache; returns how many moved."""
+        used = sorted({b for q in self.running.values() for b in q.blocks})
+        holes = sorted(set(range(len(used))) - set(used))
+        to = dict(zip([b for b in used if b >= len(used)], holes))
+        self._copy(list(to.items()))
+        for q in self.running.values():
+            q.blocks = [to.get(b, b) for b in q.blocks]
+        self.shared = {to.get(b, b): n for b, n in self.shared.items()}
+        self.free = list(range(len(used), len(used) + len(self.free)))[::-1]
+        return len(to)
 
     # -- an iteration
     @torch.no_grad()
@@ -132,7 +231,6 @@ class Instance:
         ``uniform`` gives the draws (default: from PyTorch's generator), the
         others are vectors as in ``instance_ops.sample``, one value a request.
         A call that raises leaves the batch and the free blocks as they were."""
-        s, t = self.shape, self.block_tokens
         prompts = list(prompts)
         if any(len(p) < 1 for p in prompts):
             raise ValueError("a prompt has at least one token")
@@ -143,60 +241,109 @@ class Instance:
             raise ValueError("nothing to do: no prompt and no running request")
         lengths = [self.running[r].length + 1 for r in decode] + [len(p) for p in prompts]
         blocks, taken = self._plan([self.running[r].blocks for r in decode] + [[] for _ in prompts], lengths)
+        blocks, taken, copies = self._own(blocks, [self.running[r].length for r in decode] + [0] * len(prompts), taken)
 
-        # what the kernels read: positions, slots, the running requests' tables, the prompts' offsets
         nd = len(decode)
-        positions, slots = [n - 1 for n in lengths[:nd]], []
-        for b, n in zip(blocks[:nd], lengths):
-            slots.append(b[(n - 1) // t] * t + (n - 1) % t)
-        for b, n in zip(blocks[nd:], lengths[nd:]):
-            at = np.arange(n)
-            positions += at.tolist()
-            slots += (np.asarray(b)[at // t] * t + at % t).tolist()
-        put = lambda v, dtype: torch.tensor(v, dtype=dtype, device="cuda")
-        positions, slots = put(positions, torch.int32), put(slots, torch.int64)
-        cached = put(lengths[:nd], torch.int32)
-        widest = max((len(b) for b in blocks[:nd]), default=0)
-        table = put([b + [0] * (widest - len(b)) for b in blocks[:nd]], torch.int32).reshape(nd, widest)
-        offsets = np.cumsum([0] + [len(p) for p in prompts])
-        longest = max((len(p) for p in prompts), default=0)
-        starts = put(offsets.tolist(), torch.int32)
-        last = put(list(range(nd)) + [nd + int(o) - 1 for o in offsets[1:]], torch.int64)
-
         x = self.embed[torch.cat([self.running[r].token for r in decode] + prompts)]
-        n = x.shape[0]
-        for layer, cache in zip(self.layers, self.cache):
-            h = _norm(x)
-            q = (h @ layer["q"]).view(n, s.heads, s.head_dim + s.key_dim)
-            kv = h @ layer["kv"]
-            latent, key = _norm(kv[:, :s.rank]), kv[:, s.rank:]
-            ops.rotary(q, positions, self.frequencies, layout=s.layout, offset=s.head_dim, out=q)
-            ops.latent_append(latent, key, positions, self.frequencies, slots, cache, layout=s.layout)
-            out = torch.empty(n, s.heads, s.value_dim, dtype=s.dtype, device="cuda")
-            if nd:  # absorbed: queries go into the latent space, values come out of it
-                inner = torch.matmul(q[:nd, :, :s.head_dim].transpose(0, 1), layer["key_up"].transpose(1, 2)).transpose(0, 1)
-                inner = torch.cat((inner, q[:nd, :, s.head_dim:]), -1)[:, None]
-                got, _ = ops.latent_decode(inner, cache, table, cached, scale=self.scale)
-                out[:nd] = torch.matmul(got[:, 0].transpose(0, 1), layer["value_up"]).transpose(0, 1)
-            if prompts:  # expanded: every head has keys and values of its own
-                keys = torch.matmul(latent[nd:], layer["key_up"]).transpose(0, 1)
-                values = torch.matmul(latent[nd:], layer["value_up"]).transpose(0, 1)
-                shared = ops.rotary(key[nd:, None], positions[nd:], self.frequencies, layout=s.layout)[:, 0]
-                ops.latent_prefill(q[nd:], keys, shared, values, starts, starts, scale=self.scale, longest=longest, out=out[nd:])
-            x = x + out.flatten(1) @ layer["out"]
-            if self.feed_forward is not None:
-                x = self.feed_forward(x)
+        self._copy(copies)
+        x = self._forward(x, blocks, lengths, nd, 1, prompts)
+        offsets = np.cumsum([0] + [len(p) for p in prompts])
+        last = torch.tensor(list(range(nd)) + [nd + int(o) - 1 for o in offsets[1:]], dtype=torch.int64, device="cuda")
         logits = _norm(x[last]) @ self.unembed
         if uniform is None:
             uniform = torch.rand(len(logits), device="cuda")
         tokens, logprob = ops.sample(logits, uniform, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
         # everything is queued: the batch changes now
         del self.free[len(self.free) - taken:]
+        self._give_back([b for b, _ in copies])
         ids = decode + list(range(self._next, self._next + len(prompts)))
         self._next += len(prompts)
         for i, (r, b, n) in enumerate(zip(ids, blocks, lengths)):
             self.running[r] = Running(b, n, tokens[i:i + 1])
         return ids, tokens, logprob
+
+    @torch.no_grad()
+    def speculate(self, drafts: torch.Tensor, *, draft: torch.Tensor | None = None, uniform: torch.Tensor | None = None, temperature=None):
+        """One iteration in which every running request advances by its last
+        token and as many of its drafted ones (int64 [requests, n]) as
+        ``instance_ops.verify`` accepts, with the token that follows them.  ``draft``, ``uniform`` and
+        ``temperature`` as there (default: certain drafts, draws from PyTorch's generator).  Returns (requests,
+        tokens [requests, n + 1], -1 behind each request's; how many, on the host; log-probabilities).
+        A call that raises leaves the batch and the free blocks as they were."""
+        ids = list(self.running)
+        if drafts.dim() != 2 or drafts.shape[0] != len(ids) or not ids:
+            raise ValueError("drafts must be [running requests, n], and a request must be running")
+        new = drafts.shape[1] + 1
+        held = [self.running[r].length for r in ids]
+        lengths = [n + new for n in held]
+        blocks, taken = self._plan([self.running[r].blocks for r in ids], lengths)
+        blocks, taken, copies = self._own(blocks, held, taken)
+        x = self.embed[torch.cat((torch.stack([self.running[r].token for r in ids]), drafts), 1).flatten()]
+        self._copy(copies)
+        x = self._forward(x, blocks, lengths, len(ids), new, [])
+        target = (_norm(x) @ self.unembed).view(len(ids), new, -1)
+        if uniform is None:
+            uniform = torch.rand(len(ids), new, device="cuda")
+        tokens, count, logprob = ops.verify(target, drafts.contiguous(), uniform, draft=draft, temperature=temperature)
+        counts = count.tolist()
+        del self.free[len(self.free) - taken:]
+        self._give_back([b for b, _ in copies])
+        for i, (r, b, n) in enumerate(zip(ids, blocks, held)):
+            self.running[r] = Running(b, lengths[i], tokens[i, counts[i] - 1:counts[i]])
+            self.rewind(r, n + counts[i])
+        return ids, tokens, counts, logprob
+
+    def _forward(self, x, blocks, lengths, nd, new, prompts):
+        """The layers over ``nd`` requests' last ``new`` tokens each, then the
+        prompts; ``lengths`` counts every request's tokens with them."""
+        s, t, n = self.shape, self.block_tokens, x.shape[0]
+        # what the kernels read: positions, slots, the running requests' tables, the prompts' offsets
+        positions, slots = [], []
+        for b, k, count in zip(blocks, lengths, [new] * nd + [len(p) for p in prompts]):
+            at = np.arange(k - count, k)
+            positions += at.tolist()
+            slots += (np.asarray(b)[at // t] * t + at % t).tolist()
+        put = lambda v, dtype: torch.tensor(v, dtype=dtype, device="cuda")
+        positions, slots = put(positions, torch.int32), put(slots, torch.int64)
+        every = put(lengths, torch.int32)
+        quantized = self.scales is not None
+        named = blocks if quantized else blocks[:nd]
+        widest = max((len(b) for b in named), default=0)
+        table = put([b + [0] * (widest - len(b)) for b in named], torch.int32).reshape(len(named), widest)
+        offsets = np.cumsum([0] + [len(p) for p in prompts])
+        longest = max((len(p) for p in prompts), default=0)
+        starts = put(offsets.tolist(), torch.int32)
+        rows = nd * new
+        all_starts = put([new * i for i in range(nd)] + (rows + offsets).tolist(), torch.int32)
+        for i, (layer, cache) in enumerate(zip(self.layers, self.cache)):
+            h = _norm(x)
+            q = (h @ layer["q"]).view(n, s.heads, s.head_dim + s.key_dim)
+            kv = h @ layer["kv"]
+            latent, key = _norm(kv[:, :s.rank]), kv[:, s.rank:]
+            ops.rotary(q, positions, self.frequencies, layout=s.layout, offset=s.head_dim, out=q)
+            if quantized:
+                ops.quantized_append(latent, key, self.frequencies, all_starts, table, every, cache, self.scales[i], layout=s.layout)
+            else:
+                ops.latent_append(latent, key, positions, self.frequencies, slots, cache, layout=s.layout)
+            out = torch.empty(n, s.heads, s.value_dim, dtype=s.dtype, device="cuda")
+            if nd:  # absorbed: queries go into the latent space, values come out of it
+                inner = torch.matmul(q[:rows, :, :s.head_dim].transpose(0, 1), layer["key_up"].transpose(1, 2)).transpose(0, 1)
+                inner = torch.cat((inner, q[:rows, :, s.head_dim:]), -1).unflatten(0, (nd, new))
+                got = torch.empty(nd, new, s.heads, s.rank, dtype=s.dtype, device="cuda")
+                if quantized:
+                    ops.quantized_decode(inner, cache, self.scales[i], table[:nd], every[:nd], scale=self.scale, out=got)
+                else:
+                    ops.latent_decode(inner, cache, table, every[:nd], scale=self.scale, out=got)
+                out[:rows] = torch.matmul(got.flatten(0, 1).transpose(0, 1), layer["value_up"]).transpose(0, 1)
+            if prompts:  # expanded: every head has keys and values of its own
+                keys = torch.matmul(latent[rows:], layer["key_up"]).transpose(0, 1)
+                values = torch.matmul(latent[rows:], layer["value_up"]).transpose(0, 1)
+                shared = ops.rotary(key[rows:, None], positions[rows:], self.frequencies, layout=s.layout)[:, 0]
+                ops.latent_prefill(q[rows:], keys, shared, values, starts, starts, scale=self.scale, longest=longest, out=out[rows:])
+            x = x + out.flatten(1) @ layer["out"]
+            if self.feed_forward is not None:
+                x = self.feed_forward(x)
+        return x
 
 
 def measure(node: Instance, *, prefill_tokens=(0, 256, 1024, 4096), decodes=(0, 8, 32, 63), context: int = 512, repeats: int = 3):
