@@ -88,7 +88,7 @@ struct Args {
 template <int R> struct Barriers {
     uint64_t full[kMostStages], empty[kMostStages], q_full, q_empty, s_ready[2], p_ready[2], pv_done[2], o_free;
     uint32_t tmem;
-    int first_request, first_unit, total;
+    int first_request, first_unit, total, late;
     float2 scale[kMostStages][kTile];
     alignas(16) float factor[kPieces][R];
     alignas(16) float met[R / kGroup][4][kGroup], keep[R / kGroup][kGroup];
@@ -253,6 +253,7 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
             bar_init(smem_addr(&bars->p_ready[s]), 128 * G), bar_init(smem_addr(&bars->pv_done[s]), 1);
         }
         bar_init(smem_addr(&bars->o_free), 128 * G);
+        bars->late = 0;
         bar_init_done();
     }
     if (warp == Z::soft) tmem_alloc(smem_addr(&bars->tmem), kCols);
@@ -730,8 +731,12 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
         }
     }
     __syncwarp();
+    if (dead) bars->late = 1;
     tmem_before_sync();
     __syncthreads();
+    if (bars->late) {  // a wait ran out somewhere: the block does not end while copies may be on their way (they take microseconds)
+        for (int k = 0; k < 64; ++k) __nanosleep(100000);
+    }
     if (warp == Z::soft) tmem_free(tmem, kCols);
 }
 
