@@ -252,7 +252,9 @@ int sim_op_sample(const sim_op_sample_t *args, void *cuda_stream);
  * Rows of the block after the last written one are left as they were (with another scale: they are no cached tokens).
  * Offsets must not decrease and are bounded by tokens; rows that belong to no
  * request, tokens with an index below 0 or past the table's end and table entries outside [0, blocks)
- * write nothing.  Two requests of one call must not write the same block. */
+ * write nothing.  No two requests of one call may write the same block, nor one request a block twice.
+ * A scale that a block had is read as it is where rows are kept: one that is NaN or not above 0 stands for
+ * a block of unknown numbers, which keeps its bytes (NaN) or gets others that are as unknown. */
 typedef struct {
     const void *latent;         /* [tokens][rank] */
     const void *key;            /* [tokens][rot_dim] */
@@ -335,7 +337,7 @@ typedef struct {
     const void *target;         /* [requests][drafts + 1][vocab] */
     const void *draft;          /* [requests][drafts][vocab], the target's type, or NULL */
     const int64_t *tokens;      /* [requests][drafts] */
-    const float *uniform;       /* [requests][drafts + 1], in [0, 1) */
+    const float *uniform;       /* [requests][drafts + 1], in [0, 1); for the draw, NaN and less are 0, more is the largest below 1 */
     const float *temperature;   /* [requests] or NULL (1) */
     const int32_t *drafted;     /* [requests] or NULL; taken as at least 0 and at most drafts */
     int64_t *out;               /* [requests][drafts + 1] */

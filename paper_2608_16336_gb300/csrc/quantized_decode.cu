@@ -702,6 +702,8 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
             float inv[kGroup];
 #pragma unroll
             for (int j = 0; j < kGroup; j += 4) *(float4 *)(inv + j) = *(const float4 *)&bars->keep[g][j];
+            // (its barrier knows two phases: the sums of two tiles before must be known to be there, as those of the one before tell)
+            if (i > 0) pv_wait(i - 1);
             pv_wait(i);
             tmem_after_sync();
             T *out = (T *)a.out + w.b * a.out_request;
@@ -890,7 +892,7 @@ extern "C" int sim_op_quantized_decode(const sim_op_quantized_decode_t *a, void 
     if (!std::isfinite(a->scale)) return fail(SIM_ERR_ARG, "scale must be finite");
     const int64_t rows = (int64_t)a->new_tokens * a->heads;
     if (rows == 0 || a->requests == 0) return SIM_OK;
-    if (rows > INT32_MAX || a->requests * rows > INT32_MAX) return fail(SIM_ERR_ARG, "requests * new_tokens * heads must be below 2^31");
+    if (rows > INT32_MAX - 2 * kGroup || a->requests * rows > INT32_MAX) return fail(SIM_ERR_ARG, "requests * new_tokens * heads must be below 2^31");
     if (!a->q || !a->out || !a->lengths || (!a->table && a->table_blocks) || ((!a->cache || !a->scales) && a->blocks))
         return fail(SIM_ERR_ARG, "q, cache, scales, table, lengths and out must not be NULL");
     if (!aligned16(a->q) || !aligned16(a->cache) || !aligned16(a->out) || !even_stride(a->requests, a->q_request) ||

@@ -321,10 +321,10 @@ template <typename T> __device__ __forceinline__ void logits_at(const T *row, in
 
 // A weight that is at most 1 in whole numbers of 2^-50.
 __device__ __forceinline__ u64 units_of(float w) { return __float2ull_rz(w * 0x1p50f); }
-// floor(x * f) for 0 <= f < 1 (else 0 or x) and x below 2^63.
+// floor(x * f) for 0 <= f < 1 (else 0 or the largest below x) and x below 2^63.
 __device__ __forceinline__ u64 share_of(u64 x, float f) {
     if (!(f > 0.f)) return 0;
-    if (f >= 1.f) return x;
+    if (f >= 1.f) return x ? x - 1 : 0;
     const uint32_t b = __float_as_uint(f), e = b >> 23, m = (b & 0x7FFFFF) | (e ? 0x800000 : 0);
     const int shift = 150 - (e ? e : 1);  // f = m / 2^shift, shift >= 24
     const u64 lo = x * m, hi = __umul64hi(x, m);

@@ -265,7 +265,7 @@ class Instance:
     @torch.no_grad()
     def speculate(self, drafts: torch.Tensor, *, draft: torch.Tensor | None = None, uniform: torch.Tensor | None = None, temperature=None):
         """One iteration in which every running request advances by its last
-        token and as many of its drafted ones (int64 [requests, n]) as
+        token and as many of its drafted ones (int64 [requests, n]; -1 or another number outside the vocabulary: none) as
         ``instance_ops.verify`` accepts, with the token that follows them.  ``draft``, ``uniform`` and
         ``temperature`` as there (default: certain drafts, draws from PyTorch's generator).  Returns (requests,
         tokens [requests, n + 1], -1 behind each request's; how many, on the host; log-probabilities).
@@ -278,7 +278,7 @@ class Instance:
         lengths = [n + new for n in held]
         blocks, taken = self._plan([self.running[r].blocks for r in ids], lengths)
         blocks, taken, copies = self._own(blocks, held, taken)
-        x = self.embed[torch.cat((torch.stack([self.running[r].token for r in ids]), drafts), 1).flatten()]
+        x = self.embed[torch.cat((torch.stack([self.running[r].token for r in ids]), drafts.clamp(0, len(self.embed) - 1)), 1).flatten()]
         self._copy(copies)
         x = self._forward(x, blocks, lengths, len(ids), new, [])
         target = (_norm(x) @ self.unembed).view(len(ids), new, -1)

@@ -221,6 +221,17 @@ def test_drafted_tokens(quantized):
 
 
 @pytest.mark.gpu
+def test_drafted_tokens_outside_the_vocabulary_are_refused():
+    node = make(False)
+    node.iterate([tokens(n, n) for n in (20, 31, 100)])
+    drafts = torch.tensor([[5, -1, 7], [4000, 5, 6], [2 ** 40, -2 ** 63, 3]], device="cuda")
+    _, got, counts, lp = node.speculate(drafts, uniform=torch.zeros(3, 4, device="cuda"))
+    assert counts == [2, 1, 1] and int(got[0, 0]) == 5
+    assert ((got >= 0) & (got < 4000)).sum(1).tolist() == counts and torch.isfinite(lp[got >= 0]).all()
+    whole(node, 120)
+
+
+@pytest.mark.gpu
 def test_times_of_an_instance_with_an_8_bit_cache():
     node = make(True)
     samples = instance.measure(node, prefill_tokens=(0, 64), decodes=(0, 4, 10), context=60, repeats=1)

@@ -132,6 +132,15 @@ def test_the_ends_of_the_uniform_numbers(dtype):
     assert (count == 4).all() and (out[:, :3] == 300).all() and (out[:, 3] == 5).all()
 
 
+@pytest.mark.parametrize("u,as_if", [(1.0, 1.0 - 2.0 ** -24), (7.5, 1.0 - 2.0 ** -24), (math.inf, 1.0 - 2.0 ** -24), (-0.5, 0.0), (-math.inf, 0.0), (math.nan, 0.0)])
+def test_a_draw_by_a_number_outside_its_range(u, as_if):
+    """Every request gets a token, that of the nearest number in the range (NaN: of 0)."""
+    for vocab in (9, 70001):
+        target, tokens, uniform, _ = case(3, 0, vocab, BF, seed=4, spread=0.1)
+        got = ops.verify(target, tokens, uniform.fill_(u), out=torch.full((3, 1), -7, device="cuda"), count=torch.zeros(3, dtype=torch.int32, device="cuda"))
+        assert (got[1] == 1).all() and all(torch.equal(x, y) for x, y in zip(got, ops.verify(target, tokens, uniform.fill_(as_if))))
+
+
 @pytest.mark.parametrize("known", [True, False])
 def test_greedy(known):
     """A temperature of zero (or NaN, or below): the largest logit of lowest index, and tokens are accepted while they are it."""
