@@ -86,7 +86,7 @@ struct Args {
 };
 
 template <int R> struct Barriers {
-    uint64_t full[kMostStages], empty[kMostStages], q_full, q_empty, s_ready[2], p_ready[2], pv_done[2], o_free;
+    uint64_t full[kMostStages], empty[kMostStages], q_full, q_empty, s_ready[2], p_ready[2], pv_done[4], o_free;
     uint32_t tmem;
     int first_request, first_unit, total, late;
     float2 scale[kMostStages][kTile];
@@ -250,8 +250,9 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
         bar_init(smem_addr(&bars->q_empty), 1);
         for (int s = 0; s < 2; ++s) {
             bar_init(smem_addr(&bars->s_ready[s]), 1);
-            bar_init(smem_addr(&bars->p_ready[s]), 128 * G), bar_init(smem_addr(&bars->pv_done[s]), 1);
+            bar_init(smem_addr(&bars->p_ready[s]), 128 * G);
         }
+        for (int s = 0; s < 4; ++s) bar_init(smem_addr(&bars->pv_done[s]), 1);
         bar_init(smem_addr(&bars->o_free), 128 * G);
         bars->late = 0;
         bar_init_done();
@@ -464,7 +465,7 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
                 for (int m = 0; m < tiles_m; ++m, c_low += kColBytes >> 4, d += Z::np)
                     products_8<kTile / 32, kHighC, high_p, 4096, 32 * 16>(d, c_low, p_low, word_p, add);
                 product_commit(smem_addr(&bars->empty[s]));
-                product_commit(smem_addr(&bars->pv_done[i & 1]));
+                product_commit(smem_addr(&bars->pv_done[i & 3]));
             };
             // One thread does it all.  When a tile's weights are there, the scores of the next but one are queued (S^T's
             // buffer is free: the weights were made from it), then this tile's sums, so that the next
@@ -518,7 +519,9 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
         const uint32_t s_at = tmem + Z::s_at + lanes + g * QT * kGroup, o_at = tmem + lanes + g * PT * kGroup;
         const bool with_key = a.width > a.rank;
-        auto pv_wait = [&](int j) { bar_await(smem_addr(&bars->pv_done[j & 1]), (j / 2) & 1, dead); };
+        // a tile's sums (a barrier tells one phase from the one before only: those of four tiles before are known to be there, as
+        // a tile's scores come after the sums of three before)
+        auto pv_wait = [&](int j) { bar_await(smem_addr(&bars->pv_done[j & 3]), (j / 4) & 1, dead); };
         auto larger = [](float x, float z) { return fmaxf(x, z); };
         auto added = [](float x, float z) { return x + z; };
         int later[4];
@@ -702,8 +705,6 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
             float inv[kGroup];
 #pragma unroll
             for (int j = 0; j < kGroup; j += 4) *(float4 *)(inv + j) = *(const float4 *)&bars->keep[g][j];
-            // (its barrier knows two phases: the sums of two tiles before must be known to be there, as those of the one before tell)
-            if (i > 0) pv_wait(i - 1);
             pv_wait(i);
             tmem_after_sync();
             T *out = (T *)a.out + w.b * a.out_request;
