@@ -137,8 +137,9 @@ template <> struct Held<__nv_bfloat16> {
         return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
     }
     __device__ static u64 pair(const uint4 &x, int i) {
-        const uint32_t w = (&x.x)[i];
-        return pair_of(fmaxf(__uint_as_float(w << 16), low), fmaxf(__uint_as_float(w & 0xFFFF0000u), low));
+        const __nv_bfloat162 m = __hmax2(*(const __nv_bfloat162 *)(&x.x + i), __float2bfloat162_rn(low));
+        const uint32_t w = *(const uint32_t *)&m;
+        return pair_of(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
     }
 };
 template <> struct Held<__half> {
@@ -149,8 +150,8 @@ template <> struct Held<__half> {
         return fmaxf(f.x, f.y);
     }
     __device__ static u64 pair(const uint4 &x, int i) {
-        const float2 f = __half22float2(*(const __half2 *)(&x.x + i));
-        return pair_of(fmaxf(f.x, low), fmaxf(f.y, low));
+        const float2 f = __half22float2(__hmax2(*(const __half2 *)(&x.x + i), __float2half2_rn(low)));
+        return pair_of(f.x, f.y);
     }
 };
 template <> struct Held<float> {
@@ -554,15 +555,35 @@ Cut cut_for(int sms, int64_t requests, int drafts, bool known, int vocab) {
     return c;
 }
 
-template <typename T> int run(const sim_op_verify_t *a, const Cut &c, int sms, cudaStream_t st) {
+// How many clusters of `blocks` blocks of k_draw the device runs at once (0: it cannot be asked).
+template <typename T> int clusters_at_once(int blocks) {
+    static std::atomic<int> known[64][kMostCluster + 1];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev < 64 && (n = known[dev][blocks].load(std::memory_order_relaxed))) return n;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = blocks, at.val.clusterDim.y = 1, at.val.clusterDim.z = 1;
+    cfg.gridDim = dim3(blocks), cfg.blockDim = dim3(kThreads), cfg.attrs = &at, cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, k_draw<T>, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        return 0;
+    }
+    if (dev < 64) known[dev][blocks].store(n, std::memory_order_relaxed);
+    return n;
+}
+
+template <typename T> int run(const sim_op_verify_t *a, const Cut &c, cudaStream_t st) {
     constexpr int N = Vec<T>::N;
     const int chunk_len = ((a->vocab + N - 1 + c.chunks - 1) / c.chunks + N - 1) / N * N;  // positions, which begin up to N - 1 before the row
     Stat *stats = (Stat *)a->workspace;
     cudaError_t e = launch_early(k_rows<T>, (unsigned)(a->requests * (int64_t)c.rows * c.chunks), kThreads, 0, 1, st, *a, stats, c.rows, c.chunks, chunk_len);
     if (e != cudaSuccess) return launched("sim_op_verify (rows)", e);
-    // as many blocks as run at once, of 4,096 logits at least
+    // as many blocks as run at once, of 4,096 logits at least.  (A cluster has its place within a part of the device: 37 of 8
+    // blocks do not all find one where 296 blocks would, and took 23.8 us, of 4 19.4; 64 of 4 do, and take 50.1, of 2 61.4.)
     int blocks = 1;
-    while (blocks < kMostCluster && a->vocab > blocks * 4096 && 2 * blocks * (int64_t)a->requests <= 2 * sms) blocks *= 2;
+    while (blocks < kMostCluster && a->vocab > blocks * 4096 && a->requests <= clusters_at_once<T>(2 * blocks)) blocks *= 2;
     const int step = 32 * N, parts = blocks * kWarps, stretch = ((a->vocab + N - 1 + parts - 1) / parts + step - 1) / step * step;
     e = launch_early(k_draw<T>, (unsigned)(a->requests * (int64_t)blocks), kThreads, 0, blocks, st, *a, (const Stat *)stats, c.rows, c.chunks, stretch);
     return launched("sim_op_verify (draw)", e);
@@ -600,6 +621,6 @@ extern "C" int sim_op_verify(const sim_op_verify_t *a, void *stream) {
         return fail(SIM_ERR_ARG, "requests * rows is too large");
     if (a->workspace_bytes < c.bytes) return fail(SIM_ERR_ARG, "the workspace must have %zu bytes", c.bytes);
     const cudaStream_t st = (cudaStream_t)stream;
-    if (a->type == SIM_OP_BF16) return run<__nv_bfloat16>(a, c, sms, st);
-    return a->type == SIM_OP_FP16 ? run<__half>(a, c, sms, st) : run<float>(a, c, sms, st);
+    if (a->type == SIM_OP_BF16) return run<__nv_bfloat16>(a, c, st);
+    return a->type == SIM_OP_FP16 ? run<__half>(a, c, st) : run<float>(a, c, st);
 }
