@@ -4,7 +4,8 @@ Submodules:
   workloads -- seeded synthetic inputs (cluster, tier tables, traces)
   mtsim     -- ctypes binding of the C-ABI library libmtsim.so
   instance_ops -- the operators of an instance's iteration (rotary positions,
-               cache writes, latent attention, sampling) on CUDA tensors
+               cache writes, latent attention, sampling; 8-bit caches, drafted
+               tokens, copies of cache blocks) on CUDA tensors
   instance  -- an instance that runs them, and iteration times measured on it
 Importing the package loads no native code.
 
