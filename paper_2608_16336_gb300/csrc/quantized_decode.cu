@@ -27,14 +27,15 @@ namespace {
 // that the running maximum is that of the products and they keep the type's range, and the
 // softmax's sum takes each divided by a again.
 //
-// Bound by latencies, a tile's way from scores to weights to sums (1,000 cycles) and the
-// steps of the one thread that queues the products (1,700 cycles, of which the products take 950 to 1,080): without
-// products, copies and maxima taken anew 64 requests of 200 to 10,240 tokens, 128 heads would take 103 us of 134 (before requests'
-// costs were counted in the parts, now 114: 122 MB, 50 GFLOP).  3 requests of 90,001 to 130,000 tokens, two new ones, 16 heads (204 MB) 82 us.
-// Tiles of 128 tokens have half the steps, but two stages are too few: 161 and 118 us.
+// Bound by shared memory, of whose 128 bytes a cycle a tile of 32 rows and 576 bytes a token takes 1,390 cycles' worth (the copy 290, C 580, once
+// for the scores and once for the sums, Q 290, P 190 and its way there), and by the steps of the one thread that queues the
+// products (1,700 cycles a tile).  64 requests of 200 to 10,240 tokens, 128 heads (122 MB, 50 GFLOP): 114.5 us, 134 before requests'
+// costs were counted in the parts.  3 requests of 90,001 to 130,000 tokens, two new ones, 16 heads (204 MB): 81.
+// Tiles of 128 tokens read Q half as often and have half the steps, but two stages are too few: 161 and 118 us.
 constexpr int kTile = 64, kUnit = 32;   // tokens of a tile, and of what a part may begin and end with
 constexpr int kColBytes = kTile * 128;  // a stage's column block: 64 tokens x 128 bytes
-constexpr int kGroup = 16;              // rows of a warpgroup
+constexpr int kSide = 16;               // rows side by side in a term of P
+constexpr int kGroup = 8;               // rows of a warpgroup (16: a longer chain from scores to weights, 82.7 us for the long requests, 14.0 instead of 13.0 for one of 777 tokens)
 constexpr int kWeights = 3;             // buffers of P
 constexpr int kMostStages = 8;
 constexpr int kShared = 227 * 1024;
@@ -95,9 +96,6 @@ template <int R> struct Barriers {
     int64_t to[R];
     int later[R];  // new tokens after the row's own one
 };
-// A lane's rows in S^T are 2q, 2q + 1, 8 + 2q and 9 + 2q, with q = lane % 4; they lie side by side in P, and so in O^T: column j is row
-__host__ __device__ constexpr int row_of(int j) { return j / 4 * 2 + j % 2 + (j & 2 ? 8 : 0); }
-
 __device__ __forceinline__ int tokens_of(const Args &a, int b) { return (int)min(max((int64_t)a.lengths[b], (int64_t)0), a.most); }
 // A request's stretch on the line of all requests, which is cut into the blocks' parts: its units, after
 // as many as a request costs a part besides (its queries, the first tile's start, its sums' way out: 8 us, a tile takes 1).
@@ -147,26 +145,21 @@ struct Walk {
     }
 };
 
-// 16 columns of the warp's 32 lanes.
-__device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t *r) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                 : "r"(at)
-                 : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t *r) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]), "r"(r[1]),
-                 "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
-                 "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(at)
-                 : "memory");
-}
-// 16 columns of 16 lanes, as tmem_ld_rows gives 32 and 64.
-__device__ __forceinline__ void tmem_ld_rows16(uint32_t at, uint32_t *r) {
-    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+// 8 columns of the warp's 32 lanes.
+__device__ __forceinline__ void tmem_ld8(uint32_t at, uint32_t *r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                  : "r"(at)
                  : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t *r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
+                 "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(at)
+                 : "memory");
+}
+// 8 columns of 16 lanes: a lane has columns 2q and 2q + 1, q = lane % 4, of lane / 4 and of 8 further.
+__device__ __forceinline__ void tmem_ld_rows8(uint32_t at, uint32_t *r) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
 
 // Products of 8-bit floats into 32-bit sums.  C is in 128-byte-swizzled rows, a token
@@ -212,12 +205,12 @@ template <typename T> __device__ __forceinline__ uint32_t size_bits(uint32_t two
     return __float_as_uint(elem<T>::to(v)) & 0x7FFFFFFF;
 }
 
-// A lane's four rows, joined over the lanes that have them too.
-template <typename F> __device__ __forceinline__ void join4(float *v, F f) {
+// A lane's two rows, joined over the lanes that have them too.
+template <typename F> __device__ __forceinline__ void join2(float *v, F f) {
 #pragma unroll
     for (int bit = 4; bit < 32; bit *= 2)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = f(v[e], __shfl_xor_sync(~0u, v[e], bit));
+        for (int e = 0; e < 2; ++e) v[e] = f(v[e], __shfl_xor_sync(~0u, v[e], bit));
 }
 
 // A byte that is NaN becomes zero: the weight of a row that does not see it is 0, and 0 times NaN is not.
@@ -355,7 +348,7 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
                 const float by = __uint_as_float((uint32_t)(up + 127) << 23), back = __uint_as_float((uint32_t)(127 - up) << 23);
                 // infinities and NaN: the row is NaN
                 if (lane == 0) bars->factor[k % kPieces][r] = most < 0x7F800000u ? a.scale_log2 * back : NAN;
-                uint32_t to = q_at + lane / 2 * Z::chunk + (r / kGroup * QT * kGroup + r % kGroup) * 16 + lane % 2 * 8;
+                uint32_t to = q_at + lane / 2 * Z::chunk + (r / kSide * QT * kSide + r % kSide) * 16 + lane % 2 * 8;
 #pragma unroll 1
                 for (int j = lane; j < vectors; j += 32, to += 16 * Z::chunk) {
                     float f[8];
@@ -373,7 +366,7 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
                             f[e] = (f[e] - u.x) * 16.f, f[e + 1] = (f[e + 1] - u.y) * 16.f;
                             f[e + 2] = (f[e + 2] - z.x) * 16.f, f[e + 3] = (f[e + 3] - z.y) * 16.f;
                         }
-                        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + t * kGroup * 16), "r"(word[0]), "r"(word[1]) : "memory");
+                        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + t * kSide * 16), "r"(word[0]), "r"(word[1]) : "memory");
                     }
                     x[0] = x[1], x[1] = x[2];
                 }
@@ -514,65 +507,60 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
         }
     } else {
         // ------------------------------------------------- weights and sums
-        // a lane has two tokens, 8 apart, and four rows
+        // a lane has two tokens, 8 apart, and two rows
         const int g = warp / 4, q = lane % 4, t0 = warp % 4 * 16 + lane / 4;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
-        const uint32_t s_at = tmem + Z::s_at + lanes + g * QT * kGroup, o_at = tmem + lanes + g * PT * kGroup;
+        const uint32_t side = g % 2 * kGroup, s_at = tmem + Z::s_at + lanes + g / 2 * QT * kSide + side, o_at = tmem + lanes + g / 2 * PT * kSide + side;
         const bool with_key = a.width > a.rank;
         // a tile's sums (a barrier tells one phase from the one before only: those of four tiles before are known to be there, as
         // a tile's scores come after the sums of three before)
         auto pv_wait = [&](int j) { bar_await(smem_addr(&bars->pv_done[j & 3]), (j / 4) & 1, dead); };
         auto larger = [](float x, float z) { return fmaxf(x, z); };
         auto added = [](float x, float z) { return x + z; };
-        int later[4];
+        int later[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) later[e] = bars->later[g * kGroup + row_of(4 * q + e)];
-        float base[4], sum[4];
+        for (int e = 0; e < 2; ++e) later[e] = bars->later[g * kGroup + 2 * q + e];
+        float base[2], sum[2];
         int stage = 0, buffer = 0;
         uint32_t round = 0;
         for (int i = 0; w.more; ++i) {
             if (w.u == w.u0) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) base[e] = kNothing, sum[e] = 0.f;
+                for (int e = 0; e < 2; ++e) base[e] = kNothing, sum[e] = 0.f;
             }
             const int tokens = w.tokens, fewest = tokens - a.new_tokens + 1, j0 = kUnit * w.u, past = w.past();
-            float y[2][4], per_sl[2];
+            float y[2][2], per_sl[2];
             {
                 bar_await(smem_addr(&bars->s_ready[i & 1]), (i / 2) & 1, dead);
                 tmem_after_sync();
-                // [term][rows 0..7, 8..15][token, 8 tokens on][two rows]
-                uint32_t l[QT * 8], c[QT * 8];
+                // [term][token, 8 tokens on][two rows]
+                uint32_t l[QT][4], c[QT][4];
                 const uint32_t from = s_at + (i & 1 ? kUpper : 0);
-                tmem_ld_rows<32>(from, l);
-                if (QT == 3) tmem_ld_rows16(from + 32, l + 16);
+#pragma unroll
+                for (int t = 0; t < QT; ++t) tmem_ld_rows8(from + t * kSide, l[t]);
                 if (with_key) {
-                    tmem_ld_rows<32>(from + Z::nq, c);
-                    if (QT == 3) tmem_ld_rows16(from + Z::nq + 32, c + 16);
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) tmem_ld_rows8(from + Z::nq + t * kSide, c[t]);
                 }
-                float2 f[2];
-                const float *factor = &bars->factor[w.piece % kPieces][g * kGroup];
-                f[0] = *(const float2 *)(factor + 2 * q), f[1] = *(const float2 *)(factor + 8 + 2 * q);
+                const float2 f = *(const float2 *)&bars->factor[w.piece % kPieces][g * kGroup + 2 * q];
                 const float2 scale[2] = {bars->scale[stage][t0], bars->scale[stage][t0 + 8]};
                 tmem_wait_ld();
 #pragma unroll
                 for (int d = 0; d < 2; ++d) {
                     const float sl = scale[d].x, sk = scale[d].y, log_sl = __log2f(sl);
                     per_sl[d] = exp2_fast(-log_sl);
+                    auto term = [&](const uint32_t *x, int r) { return __uint_as_float(x[d * 2 + r]); };
+                    float u0 = term(l[QT - 1], 0), u1 = term(l[QT - 1], 1), v0 = 0.f, v1 = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        auto term = [&](const uint32_t *x, int t, int r) { return __uint_as_float(x[t * 8 + e * 4 + d * 2 + r]); };
-                        float u0 = term(l, QT - 1, 0), u1 = term(l, QT - 1, 1), v0 = 0.f, v1 = 0.f;
+                    for (int t = QT - 2; t >= 0; --t) fma2(u0, u1, u0, u1, 0.0625f, 0.0625f, term(l[t], 0), term(l[t], 1));
+                    if (with_key) {
+                        v0 = term(c[QT - 1], 0), v1 = term(c[QT - 1], 1);
 #pragma unroll
-                        for (int t = QT - 2; t >= 0; --t) fma2(u0, u1, u0, u1, 0.0625f, 0.0625f, term(l, t, 0), term(l, t, 1));
-                        if (with_key) {
-                            v0 = term(c, QT - 1, 0), v1 = term(c, QT - 1, 1);
-#pragma unroll
-                            for (int t = QT - 2; t >= 0; --t) fma2(v0, v1, v0, v1, 0.0625f, 0.0625f, term(c, t, 0), term(c, t, 1));
-                            v0 *= sk, v1 *= sk;
-                        }
-                        fma2(u0, u1, u0, u1, sl, sl, v0, v1);
-                        fma2(y[d][2 * e], y[d][2 * e + 1], u0, u1, f[e].x, f[e].y, log_sl, log_sl);
+                        for (int t = QT - 2; t >= 0; --t) fma2(v0, v1, v0, v1, 0.0625f, 0.0625f, term(c[t], 0), term(c[t], 1));
+                        v0 *= sk, v1 *= sk;
                     }
+                    fma2(u0, u1, u0, u1, sl, sl, v0, v1);
+                    fma2(y[d][0], y[d][1], u0, u1, f.x, f.y, log_sl, log_sl);
                 }
             }
             if (j0 + kTile > min(fewest, past)) {
@@ -580,7 +568,7 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
                 for (int d = 0; d < 2; ++d) {
                     const int j = j0 + t0 + 8 * d;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                    for (int e = 0; e < 2; ++e)
                         if (j >= past || j >= tokens - later[e]) y[d][e] = -INFINITY;
                 }
                 // cached rows that not all of the block's rows see, and those that came with the last ones, without NaN
@@ -595,34 +583,34 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
                         *at = make_uint4(without_nan(v.x), without_nan(v.y), without_nan(v.z), without_nan(v.w));
                     }
             }
-            float x[2][4], most = -INFINITY;
+            float x[2][2], most = -INFINITY;
 #pragma unroll
             for (int d = 0; d < 2; ++d)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[d][e] = y[d][e] + base[e], most = fmaxf(most, x[d][e]);
+                for (int e = 0; e < 2; ++e) x[d][e] = y[d][e] + base[e], most = fmaxf(most, x[d][e]);
             if (group_any(g, most > kLimit)) {
                 // a maximum anew, of the whole group's tokens
-                float v[4], keep[4];
+                float v[2], keep[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = fmaxf(y[0][e], y[1][e]);
-                join4(v, larger);
-                if (lane < 4) *(float4 *)&bars->met[g][warp % 4][4 * q] = make_float4(v[0], v[1], v[2], v[3]);
+                for (int e = 0; e < 2; ++e) v[e] = fmaxf(y[0][e], y[1][e]);
+                join2(v, larger);
+                if (lane < 4) *(float2 *)&bars->met[g][warp % 4][2 * q] = make_float2(v[0], v[1]);
                 group_sync(g);
-                float4 m = *(const float4 *)&bars->met[g][0][4 * q];
+                float2 m = *(const float2 *)&bars->met[g][0][2 * q];
 #pragma unroll
                 for (int k = 1; k < 4; ++k) {
-                    const float4 o = *(const float4 *)&bars->met[g][k][4 * q];
-                    m.x = fmaxf(m.x, o.x), m.y = fmaxf(m.y, o.y), m.z = fmaxf(m.z, o.z), m.w = fmaxf(m.w, o.w);
+                    const float2 o = *(const float2 *)&bars->met[g][k][2 * q];
+                    m.x = fmaxf(m.x, o.x), m.y = fmaxf(m.y, o.y);
                 }
-                const float high[4] = {m.x, m.y, m.z, m.w};
+                const float high[2] = {m.x, m.y};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < 2; ++e) {
                     const float anew = high[e] + base[e] > kLimit ? kRaise - high[e] : base[e];
                     keep[e] = anew == base[e] ? 1.f : exp2_fast(anew - base[e]);
                     base[e] = anew, sum[e] *= keep[e], x[0][e] = y[0][e] + anew, x[1][e] = y[1][e] + anew;
                 }
                 if (w.u > w.u0) {
-                    if (warp % 4 == 0 && lane < 4) *(float4 *)&bars->keep[g][4 * q] = make_float4(keep[0], keep[1], keep[2], keep[3]);
+                    if (warp % 4 == 0 && lane < 4) *(float2 *)&bars->keep[g][2 * q] = make_float2(keep[0], keep[1]);
                     group_sync(g);
                     pv_wait(i - 1);
                     tmem_after_sync();
@@ -633,40 +621,34 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
                     for (int m = 0; m < tiles_m; ++m) {
                         uint32_t o[PT][kGroup];
 #pragma unroll
-                        for (int t = 0; t < PT; ++t) tmem_ld16(o_at + m * Z::np + t * kGroup, o[t]);
+                        for (int t = 0; t < PT; ++t) tmem_ld8(o_at + m * Z::np + t * kSide, o[t]);
                         tmem_wait_ld();
 #pragma unroll
                         for (int t = 0; t < PT; ++t) {
 #pragma unroll
                             for (int r = 0; r < kGroup; ++r) o[t][r] = __float_as_uint(__uint_as_float(o[t][r]) * k[r]);
-                            tmem_st16(o_at + m * Z::np + t * kGroup, o[t]);
+                            tmem_st8(o_at + m * Z::np + t * kSide, o[t]);
                         }
                     }
                     tmem_wait_st();
                 }
             }
-            uint32_t h[2][2];
+            uint32_t h[2];
 #pragma unroll
-            for (int d = 0; d < 2; ++d)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float p0 = exp2_fast(x[d][2 * e]), p1 = exp2_fast(x[d][2 * e + 1]);
-                    fma2(sum[2 * e], sum[2 * e + 1], p0, p1, per_sl[d], per_sl[d], sum[2 * e], sum[2 * e + 1]);
-                    h[d][e] = pack2<__half>(p0, p1);
-                }
-            const uint32_t to = p_at + buffer * Z::p_bytes + g * PT * (kTile * 16) + t0 * 16 + 4 * q;
+            for (int d = 0; d < 2; ++d) {
+                const float p0 = exp2_fast(x[d][0]), p1 = exp2_fast(x[d][1]);
+                fma2(sum[0], sum[1], p0, p1, per_sl[d], per_sl[d], sum[0], sum[1]);
+                h[d] = pack2<__half>(p0, p1);
+            }
+            const uint32_t to = p_at + buffer * Z::p_bytes + g / 2 * PT * (kTile * 16) + t0 * 16 + side + 2 * q;
 #pragma unroll
             for (int t = 0; t < PT; ++t)
 #pragma unroll
                 for (int d = 0; d < 2; ++d) {
-                    uint32_t top[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        top[e] = (h[d][e] + 0x00800080u) & 0xFF00FF00u;  // the upper byte, rounded
-                        const __half2 rest = __hsub2(*(const __half2 *)&h[d][e], *(const __half2 *)&top[e]);
-                        *(__half2 *)&h[d][e] = __hmul2(rest, __floats2half2_rn(8.f, 8.f));
-                    }
-                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + t * (kTile * 16) + d * 128), "r"(__byte_perm(top[0], top[1], 0x7531)) : "memory");
+                    const uint32_t top = (h[d] + 0x00800080u) & 0xFF00FF00u;  // the upper byte, rounded
+                    const __half2 rest = __hsub2(*(const __half2 *)&h[d], *(const __half2 *)&top);
+                    *(__half2 *)&h[d] = __hmul2(rest, __floats2half2_rn(8.f, 8.f));
+                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + t * (kTile * 16) + d * 128), "h"((uint16_t)__byte_perm(top, 0, 0x4431)) : "memory");
                 }
             fence_async();
             tmem_before_sync();
@@ -678,9 +660,9 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
                 continue;
             }
             // ------------------------------------------- the piece's end
-            join4(sum, added);
+            join2(sum, added);
             group_sync(g);  // what met before has been read
-            if (lane < 4) *(float4 *)&bars->met[g][warp % 4][4 * q] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            if (lane < 4) *(float2 *)&bars->met[g][warp % 4][2 * q] = make_float2(sum[0], sum[1]);
             group_sync(g);
             const bool whole = w.u0 == 0 && w.u1 == w.n;
             // an unfinished piece: the part's last if it begins the request, else its first
@@ -688,18 +670,18 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
             const int mine = min(kGroup, here - g * kGroup);
             if (warp % 4 == 0 && lane < 4) {
                 // the rows' statistics; what their sums are multiplied with stays behind for the others
-                float inv[4];
+                float inv[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = 4 * q + e, r = row_of(j);
-                    const float all = (bars->met[g][0][j] + bars->met[g][1][j]) + (bars->met[g][2][j] + bars->met[g][3][j]);
+                for (int e = 0; e < 2; ++e) {
+                    const int r = 2 * q + e;
+                    const float all = (bars->met[g][0][r] + bars->met[g][1][r]) + (bars->met[g][2][r] + bars->met[g][3][r]);
                     inv[e] = all != 0.f ? 1.f / all : 0.f;
                     if (r < mine) {
                         if (!whole) a.stats[slot * R + g * kGroup + r] = make_float2(base[e], all);
                         else if (a.lse) a.lse[(int64_t)w.b * rows + rt * R + g * kGroup + r] = all != 0.f ? (log2f(all) - base[e]) * 0.6931471805599453f : -INFINITY;
                     }
                 }
-                *(float4 *)&bars->keep[g][4 * q] = make_float4(inv[0], inv[1], inv[2], inv[3]);
+                *(float2 *)&bars->keep[g][2 * q] = make_float2(inv[0], inv[1]);
             }
             group_sync(g);
             float inv[kGroup];
@@ -713,17 +695,16 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
             for (int m = 0; m < tiles_m; ++m) {
                 uint32_t o[PT][kGroup];
 #pragma unroll
-                for (int t = 0; t < PT; ++t) tmem_ld16(o_at + m * Z::np + t * kGroup, o[t]);
+                for (int t = 0; t < PT; ++t) tmem_ld8(o_at + m * Z::np + t * kSide, o[t]);
                 tmem_wait_ld();
                 const int col = 128 * m + threadIdx.x % 128;
 #pragma unroll
-                for (int j = 0; j < kGroup; ++j) {
-                    const int r = row_of(j);
-                    float v = __uint_as_float(o[PT - 1][j]);
+                for (int r = 0; r < kGroup; ++r) {
+                    float v = __uint_as_float(o[PT - 1][r]);
 #pragma unroll
-                    for (int t = PT - 2; t >= 0; --t) v = fmaf(v, 0.125f, __uint_as_float(o[t][j]));
+                    for (int t = PT - 2; t >= 0; --t) v = fmaf(v, 0.125f, __uint_as_float(o[t][r]));
                     if (r < mine && col < a.rank) {
-                        if (whole) out[bars->to[g * kGroup + r] + col] = elem<T>::from(inv[j] != 0.f ? v * inv[j] : 0.f);
+                        if (whole) out[bars->to[g * kGroup + r] + col] = elem<T>::from(inv[r] != 0.f ? v * inv[r] : 0.f);
                         else sums[(int64_t)r * a.rank + col] = v;
                     }
                 }
@@ -840,7 +821,7 @@ Cut cut_for(int sms, int row_tile, int64_t requests, int64_t new_tokens, int64_t
 }
 
 // Rows of a block: 32 where there are so many and their sums and scores fit the tensor memory.
-int row_tile_for(bool bf16, int64_t rows) { return bf16 && rows > kGroup ? 2 * kGroup : kGroup; }
+int row_tile_for(bool bf16, int64_t rows) { return bf16 && rows > kSide ? 2 * kSide : kSide; }
 
 template <typename T, int G> int run(const Args &given, const CUtensorMap &map, const CUtensorMap &key, const Cut &c, cudaStream_t st) {
     using Z = Shape<T, G>;
@@ -876,7 +857,7 @@ extern "C" size_t sim_op_quantized_decode_workspace(int32_t requests, int32_t ne
     if (requests < 1 || new_tokens < 1 || heads < 1 || rank < 1 || (int64_t)new_tokens * heads > INT32_MAX) return 256;
     const int sms = sm_count();
     if (!sms) return 0;
-    const size_t x = cut_for(sms, kGroup, requests, new_tokens, heads, rank).bytes(), y = cut_for(sms, 2 * kGroup, requests, new_tokens, heads, rank).bytes();
+    const size_t x = cut_for(sms, kSide, requests, new_tokens, heads, rank).bytes(), y = cut_for(sms, 2 * kSide, requests, new_tokens, heads, rank).bytes();
     return x > y ? x : y;
 }
 
@@ -893,7 +874,7 @@ extern "C" int sim_op_quantized_decode(const sim_op_quantized_decode_t *a, void 
     if (!std::isfinite(a->scale)) return fail(SIM_ERR_ARG, "scale must be finite");
     const int64_t rows = (int64_t)a->new_tokens * a->heads;
     if (rows == 0 || a->requests == 0) return SIM_OK;
-    if (rows > INT32_MAX - 2 * kGroup || a->requests * rows > INT32_MAX) return fail(SIM_ERR_ARG, "requests * new_tokens * heads must be below 2^31");
+    if (rows > INT32_MAX - 2 * kSide || a->requests * rows > INT32_MAX) return fail(SIM_ERR_ARG, "requests * new_tokens * heads must be below 2^31");
     if (!a->q || !a->out || !a->lengths || (!a->table && a->table_blocks) || ((!a->cache || !a->scales) && a->blocks))
         return fail(SIM_ERR_ARG, "q, cache, scales, table, lengths and out must not be NULL");
     if (!aligned16(a->q) || !aligned16(a->cache) || !aligned16(a->out) || !even_stride(a->requests, a->q_request) ||
@@ -943,6 +924,6 @@ extern "C" int sim_op_quantized_decode(const sim_op_quantized_decode_t *a, void 
     const void *cache = a->blocks ? a->cache : a->q;
     if (!byte_box_map(&map, cache, 2, size, stride, box) || !byte_box_map(&key, cache, 2, size, stride, thin)) return SIM_ERR_CUDA;
     const cudaStream_t st = (cudaStream_t)stream;
-    if (!bf) return run<__half, 1>(k, map, key, c, st);
-    return row_tile == kGroup ? run<__nv_bfloat16, 1>(k, map, key, c, st) : run<__nv_bfloat16, 2>(k, map, key, c, st);
+    if (!bf) return run<__half, 2>(k, map, key, c, st);
+    return row_tile == kSide ? run<__nv_bfloat16, 2>(k, map, key, c, st) : run<__nv_bfloat16, 4>(k, map, key, c, st);
 }
