@@ -331,10 +331,9 @@ __device__ __forceinline__ u64 share_of(u64 x, float f) {
     const u64 lo = x * m, hi = __umul64hi(x, m);
     return shift < 64 ? hi << (64 - shift) | lo >> shift : shift < 128 ? hi >> (shift - 64) : 0;
 }
+// (Masses are shares of one row's, so that all together are less than 2^51: their upper parts fit 32 bits.)
 __device__ __forceinline__ u64 warp_total(u64 v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
-    return v;
+    return ((u64)__reduce_add_sync(~0u, (unsigned)(v >> 25)) << 25) + __reduce_add_sync(~0u, (unsigned)v & 0x1FFFFFF);
 }
 __device__ __forceinline__ u64 warp_up_to(u64 v) {
 #pragma unroll
@@ -437,10 +436,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_draw(const __grid_constant__ si
         }
     };
     auto units = [&](const float *w) {
-        float s = w[0];
+        u64 s = pair_of(w[0], w[1]);
 #pragma unroll
-        for (int e = 1; e < N; ++e) s += w[e];
-        return units_of(s);
+        for (int e = 2; e < N; e += 2) s = pair_add(s, pair_of(w[e], w[e + 1]));
+        float s0, s1;
+        parts_of(s, s0, s1);
+        return units_of(s0 + s1);
     };
     const int part = rank * kWarps + warp, begin = part * stretch, end = min(begin + stretch, end_at);
     int chosen = -1;  // the part with the point
