@@ -147,15 +147,18 @@ def _int32(name, t, shape) -> None:
 
 
 def _eight(cache, scales, width) -> tuple:
-    """The strides of an 8-bit cache with its scales."""
+    """Block and row stride, blocks and tokens of a block of an 8-bit cache with its scales."""
     if cache.dtype is not EIGHT:
         raise TypeError("cache must be float8_e4m3fn, not %s" % cache.dtype)
     if scales.dtype is not torch.float32:
         raise TypeError("scales must be float32, not %s" % scales.dtype)
-    if cache.dim() != 3:
+    shape = cache.shape
+    if len(shape) != 3:
         raise ValueError("cache must be [blocks, block_tokens, width]")
-    _packed("scales", scales, (cache.shape[0], 2))
-    return _rows("cache", cache, (cache.shape[0], cache.shape[1], width))
+    blocks, tokens, _ = shape
+    _packed("scales", scales, (blocks, 2))
+    block, row, _ = _rows("cache", cache, (blocks, tokens, width))
+    return block, row, blocks, tokens
 
 
 def _positions(t, n) -> int:
@@ -433,23 +436,24 @@ def quantized_append(latent, key, frequencies, offsets, table, lengths, cache, s
     holds rows keeps them, in a larger scale where the new rows need one.
     Returns (cache, scales)."""
     rot = _frequencies(frequencies)
-    if latent.dim() != 2 or table.dim() != 2:
+    ls, named = latent.shape, table.shape
+    if len(ls) != 2 or len(named) != 2:
         raise ValueError("latent must be [tokens, rank], table [requests, n]")
-    n, rank = latent.shape
-    b, width = table.shape
-    ls, ks = _rows("latent", latent, latent.shape), _rows("key", key, (n, rot))
-    cs = _eight(cache, scales, rank + rot)
+    n, rank = ls
+    b, width = named
+    ls, ks = _rows("latent", latent, ls), _rows("key", key, (n, rot))
+    cache_block, cache_row, blocks, block_tokens = _eight(cache, scales, rank + rot)
     _int32("offsets", offsets, (b + 1,))
     _int32("lengths", lengths, (b,))
     if table.dtype is not torch.int32:
         raise TypeError("table must be int32, not %s" % table.dtype)
-    ts = _rows("table", table, (b, width))
+    ts = _rows("table", table, named)
     code = _type("latent", latent, key)
     device = _place(latent, key, cache, scales, frequencies, offsets, table, lengths)
     rc = (_LIB or lib()).sim_op_quantized_append(
         QUANTIZED_APPEND.pack(latent.data_ptr(), key.data_ptr(), frequencies.data_ptr(), offsets.data_ptr(), table.data_ptr(),
-                              lengths.data_ptr(), cache.data_ptr(), scales.data_ptr(), n, ls[0], ks[0], cs[0], cs[1], ts[0],
-                              cache.shape[0], b, width, cache.shape[1], rank, rot, code, _layout(layout), amplitude),
+                              lengths.data_ptr(), cache.data_ptr(), scales.data_ptr(), n, ls[0], ks[0], cache_block, cache_row, ts[0],
+                              blocks, b, width, block_tokens, rank, rot, code, _layout(layout), amplitude),
         _stream_of(device))
     if rc:
         _failed(rc)
@@ -471,7 +475,7 @@ def quantized_decode(q, cache, scales, table, lengths, *, scale, out=None, lse=N
         raise ValueError("rank must be a multiple of 64 up to %d and width - rank one of 16 up to %d: %d, %d"
                          % (MAX_RANK, MAX_KEY, rank, width - rank))
     qs, os_ = _rows("q", q, q.shape), _rows("out", out, (b, new, heads, rank))
-    cs = _eight(cache, scales, width)
+    cache_block, cache_row, blocks, block_tokens = _eight(cache, scales, width)
     if table.dtype is not torch.int32:
         raise TypeError("table must be int32, not %s" % table.dtype)
     ts = _rows("table", table, (b, table.shape[1]))
@@ -496,8 +500,8 @@ def quantized_decode(q, cache, scales, table, lengths, *, scale, out=None, lse=N
     try:
         rc = L.sim_op_quantized_decode(
             QUANTIZED_DECODE.pack(q.data_ptr(), cache.data_ptr(), scales.data_ptr(), table.data_ptr(), lengths.data_ptr(), out.data_ptr(),
-                                  lse.data_ptr(), work, nbytes, qs[0], qs[1], qs[2], os_[0], os_[1], os_[2], cs[0], cs[1], ts[0],
-                                  cache.shape[0], b, new, heads, rank, width - rank, cache.shape[1], table.shape[1], code, scale),
+                                  lse.data_ptr(), work, nbytes, qs[0], qs[1], qs[2], os_[0], os_[1], os_[2], cache_block, cache_row, ts[0],
+                                  blocks, b, new, heads, rank, width - rank, block_tokens, table.shape[1], code, scale),
             stream)
     finally:
         _release(work)  # what the stream allocates next comes after this call's kernels
@@ -592,13 +596,14 @@ def block_copy(source, destination, from_blocks, to_blocks):
     number outside its tensor's blocks (-1: padding) copies nothing.  They may be one tensor when no
     block that is written is read by another pair; no two pairs may name the same
     destination.  Returns ``destination``."""
-    if source.dim() not in (3, 4) or source.dim() != destination.dim():
+    shape, there = source.shape, destination.shape
+    if len(shape) not in (3, 4) or len(shape) != len(there):
         raise ValueError("source and destination must be [layers, blocks, block_tokens, width] or [layers, blocks, width]")
     if source.dtype is not destination.dtype:
         raise TypeError("source and destination must have the same type: %s and %s" % (source.dtype, destination.dtype))
-    layers, have, *block = source.shape
-    room = destination.shape[1]
-    ss, ds = _rows("source", source, source.shape), _rows("destination", destination, (layers, room, *block))
+    layers, have, *block = shape
+    room = there[1]
+    ss, ds = _rows("source", source, shape), _rows("destination", destination, (layers, room, *block))
     n = from_blocks.shape[0] if from_blocks.dim() == 1 else -1
     if n < 0:
         raise ValueError("from_blocks must be a vector")
