@@ -13,8 +13,8 @@ namespace cg = cooperative_groups;
 // and the sum of its weights.  k_draw, a cluster of blocks a request, joins these, decides how many tokens are
 // accepted, goes once more over the one row (or the two) that the next token is drawn from, and the
 // warp whose stretch holds the point looks for it.
-// 64 requests, 4 rows of 131,075 bfloat16 logits and 3 of the draft (117 MB) take 50 us: the rows 25, bound by instructions (11 a
-// logit; 62 registers and two blocks a multiprocessor 33), the draw 22, bound by waiting for its loads.
+// 64 requests, 4 rows of 131,075 bfloat16 logits and 3 of the draft (117 MB) take 49 us: the rows 25, bound by instructions (11 a
+// logit; 62 registers and two blocks a multiprocessor 33), the draw 21, bound by waiting for its loads.
 //
 // Nothing is in 64-bit floating point, which runs at a sixtieth of the rate here (a division by every thread took
 // 58 of 165 us).  Sums of single threads and warps are 32-bit floats, whose errors are independent and average out; sums
