@@ -14,11 +14,17 @@ __device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ float2 unpack_e4m3(uint32_t two) {
+__device__ __forceinline__ uint32_t pack_e4m3(__half2 x) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*(uint32_t *)&x));
+    return r;
+}
+__device__ __forceinline__ __half2 halves_of_e4m3(uint32_t two) {
     uint32_t h;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
-    return __half22float2(*(__half2 *)&h);
+    return *(__half2 *)&h;
 }
+__device__ __forceinline__ float2 unpack_e4m3(uint32_t two) { return __half22float2(halves_of_e4m3(two)); }
 
 // The smallest power of two in range with a <= 448 times it: 448 is 1.75 * 2^8.
 __device__ __forceinline__ float scale_for(float a) {

@@ -353,20 +353,20 @@ __global__ void __launch_bounds__(Shape<T, G>::threads, 1) k_quantized_decode(co
                 for (int j = lane; j < vectors; j += 32, to += 16 * Z::chunk) {
                     float f[8];
                     ((const Vec<T> *)x)->to(f);
+                    // (up to 11 bits below 256 are a 16-bit float, and so is what a term leaves of them; one below 2^-14
+                    // is rounded by at most 2^-25, far less than the last term can tell)
+                    __half2 h[4];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) f[e] *= by;
+                    for (int e = 0; e < 4; ++e) h[e] = __floats2half2_rn(f[2 * e] * by, f[2 * e + 1] * by);
 #pragma unroll
                     for (int t = 0; t < QT; ++t) {
-                        uint32_t word[2];
+                        uint32_t two[4];
 #pragma unroll
-                        for (int e = 0; e < 8; e += 4) {
-                            const uint32_t lo = pack_e4m3(f[e], f[e + 1]), hi = pack_e4m3(f[e + 2], f[e + 3]);
-                            word[e / 4] = lo | hi << 16;
-                            const float2 u = unpack_e4m3(lo), z = unpack_e4m3(hi);
-                            f[e] = (f[e] - u.x) * 16.f, f[e + 1] = (f[e + 1] - u.y) * 16.f;
-                            f[e + 2] = (f[e + 2] - z.x) * 16.f, f[e + 3] = (f[e + 3] - z.y) * 16.f;
+                        for (int e = 0; e < 4; ++e) {
+                            two[e] = pack_e4m3(h[e]);
+                            h[e] = __hmul2(__hsub2(h[e], halves_of_e4m3(two[e])), __floats2half2_rn(16.f, 16.f));
                         }
-                        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + t * kSide * 16), "r"(word[0]), "r"(word[1]) : "memory");
+                        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + t * kSide * 16), "r"(two[0] | two[1] << 16), "r"(two[2] | two[3] << 16) : "memory");
                     }
                     x[0] = x[1], x[1] = x[2];
                 }
