@@ -306,6 +306,31 @@ def test_decode(lengths, new, heads, rank, key_dim, block, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("lengths,new,heads,rank,key_dim,block", [
+    ([100, 0, 45, 330], 40, 130, 64, 16, 16), ([90, 700], 33, 77, 128, 0, 16), ([1000], 1, 16, 512, 64, 1000), ([5000], 2, 24, 512, 64, 5003),
+    ([64 * k + 1 for k in range(140)], 1, 40, 64, 64, 16)])
+def test_decode_more_rows_than_blocks_of_threads_and_one_block_of_cache(lengths, new, heads, rank, key_dim, block, dtype):
+    q, cache, scales, table, n = decode_case(lengths, new, heads, rank, key_dim, block, dtype, seed=heads)
+    if len(lengths) == 1:  # a cache of a single block
+        i = int(table[0, 0])
+        cache, scales, table = cache[i:i + 1], scales[i:i + 1], torch.zeros_like(table)
+    scale = 1.0 / math.sqrt(rank + key_dim)
+    out, lse = ops.quantized_decode(q, cache, scales, table, n, scale=scale, out=torch.full((len(lengths), new, heads, rank), float("nan"), device="cuda", dtype=dtype))
+    check_decode(q, cache, scales, table, n, rank, scale, out, lse)
+
+
+def test_decode_without_a_cache_or_a_table():
+    q = randn(gen(3), 2, 2, 20, 576, dtype=BF)
+    none = torch.empty(0, 16, 576, device="cuda", dtype=torch.uint8).view(E4), torch.empty(0, 2, device="cuda")
+    some = torch.zeros(4, 16, 576, device="cuda", dtype=torch.uint8).view(E4), torch.ones(4, 2, device="cuda")
+    out, lse = ops.quantized_decode(q, *none, ints([[0, 1], [5, 2]]), ints([20, 1]), scale=0.1)  # blocks of zeros
+    assert not out.any() and torch.allclose(lse[0, :, 0].cpu(), torch.log(torch.tensor([19.0, 20.0])), rtol=0, atol=1e-6)
+    assert (lse[1, 0] == -math.inf).all() and (lse[1, 1] == 0).all()
+    out, lse = ops.quantized_decode(q, *some, ints([]).reshape(2, 0), ints([20, 1]), scale=0.1)  # no token can be named
+    assert not out.any() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
 def test_decode_sizes_far_apart(dtype):
     """Blocks whose scales differ by 2^24 (the large ones with few of the weights), queries of very different size, negative and zero scale."""
     q, cache, scales, table, n = decode_case([700, 700], 1, 16, 512, 64, 16, dtype, seed=9, spread=12)

@@ -116,6 +116,14 @@ def test_verify(b, d, vocab, known, dtype):
     assert all(torch.equal(x, y) for x, y in zip(got, ops.verify(target, tokens, uniform, **rest)))  # the same bits
 
 
+@pytest.mark.parametrize("b,d,dtype", [(310, 1, BF), (160, 0, F32), (90, 2, HF), (40, 1, BF), (21, 1, HF)])
+def test_verify_more_requests_than_blocks_of_threads(b, d, dtype):
+    """Every size of cluster, down to one block with more steps a warp than are kept."""
+    for known in (True, False):
+        target, tokens, uniform, draft = case(b, d, 70001, dtype, seed=b, known=known)
+        check(target, tokens, uniform, draft, None, None, *ops.verify(target, tokens, uniform, draft=draft))
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_the_ends_of_the_uniform_numbers(dtype):
     """0 accepts whatever the target can give and draws the first token; just below 1 the last."""
