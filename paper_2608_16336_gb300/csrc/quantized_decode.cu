@@ -28,8 +28,8 @@ namespace {
 // softmax's sum takes each divided by a again.
 //
 // Bound by shared memory, of whose 128 bytes a cycle a tile of 32 rows and 576 bytes a token takes 1,390 cycles' worth (the copy 290, C 580, once
-// for the scores and once for the sums, Q 290, P 190 and its way there), and by the steps of the one thread that queues the
-// products (1,700 cycles a tile).  64 requests of 200 to 10,240 tokens, 128 heads (122 MB, 50 GFLOP): 114.5 us, 134 before requests'
+// for the scores and once for the sums, Q 290, P 190 and its way there), by the way from scores to weights, which a tile's warps go one tile after another, and by
+// the steps of the one thread that queues the products (1,800 to 2,000 cycles a tile in all).  64 requests of 200 to 10,240 tokens, 128 heads (122 MB, 50 GFLOP): 114.5 us, 134 before requests'
 // costs were counted in the parts.  3 requests of 90,001 to 130,000 tokens, two new ones, 16 heads (204 MB): 81.
 // Tiles of 128 tokens read Q half as often and have half the steps, but two stages are too few: 161 and 118 us.
 constexpr int kTile = 64, kUnit = 32;   // tokens of a tile, and of what a part may begin and end with
