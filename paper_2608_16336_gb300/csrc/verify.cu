@@ -184,9 +184,9 @@ __global__ void __launch_bounds__(kThreads, 3) k_rows(const __grid_constant__ si
     const Vec<T> *x = (const Vec<T> *)(from - skip);
     float top = -INFINITY, sum = 0.f;
     int first = 0x7FFFFFFF;
-    // Without a branch for a logit's kind: -infinity and NaN count as the lowest number `low`, whose weight is 0 under any larger
-    // logit (a temperature within reason), and the largest is taken anew with every vector.  Threads that
-    // find nothing larger than that, or +infinity, look again below.
+    // Without a branch for a logit's kind: -infinity and NaN count as the lowest number `low`, whose weight is 0 under a
+    // logit far above it, and the largest is taken anew with every vector.  Threads that find nothing from which a
+    // weight at `low` would be 0 (2^-150: of float16 rows, whose lowest number is an ordinary one), or +infinity, look again below.
     const bool plain = !c.greedy && c.hi < 1e6f && c.hi > 0.01f;
     if (plain) {
         const u64 hi = pair_of(c.hi, c.hi), lo = pair_of(c.lo, c.lo);
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_rows(const __grid_constant__ si
         if (top == -INFINITY) sum = 0.f;
     }
     // one by one
-    const bool again = plain && (top == INFINITY || (top > -INFINITY && top <= Held<T>::low));
+    const bool again = plain && (top == INFINITY || (top > -INFINITY && (top - Held<T>::low) * c.hi < 150.f));
     if (again) top = -INFINITY, sum = 0.f;
     if (!plain || again) for (int p0 = begin + threadIdx.x * N; p0 < end; p0 += kBatch * kThreads * N) {
         Vec<T> v[kBatch];
