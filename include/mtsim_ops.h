@@ -321,7 +321,8 @@ size_t sim_op_quantized_decode_workspace(int32_t requests, int32_t new_tokens, i
  * With t the temperature, p_i = softmax(target_i / t) and q_i = softmax(draft_i / t):
  *   1. drafted tokens x_0, x_1, .. are accepted while uniform[i] * q_i(x_i) < p_i(x_i);
  *   2. at the first that is not, i, the next token is drawn from max(p_i - q_i, 0)
- *      scaled to a sum of one (where that is 0 everywhere: from p_i); with all accepted, from p_D;
+ *      scaled to a sum of one (where that is 0 everywhere: from p_i; rows whose sums of weights agree to
+ *      2^-20 are taken to have the same, so that equal ones leave 0 wherever they lie); with all accepted, from p_D;
  *   3. the draw takes the first token, in vocabulary order, up to which the weights sum to more
  *      than uniform[drafts] times their total.
  * So the tokens are distributed as if drawn from the target one by one.  out[b] holds

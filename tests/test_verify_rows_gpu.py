@@ -5,7 +5,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 from paper_2608_16336_gb300 import instance_ops as ops  # noqa: E402
-from test_verify_gpu import BF, F32, HF, check  # noqa: E402
+from test_verify_gpu import BF, F32, HF, check, gen  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +46,24 @@ def test_rows_whose_largest_logit_is_near_the_lowest_number(vocab, t, known, dty
         for u in (0.0, 0.9):
             uniform = torch.full((b, 2), u, device="cuda")
             check(target, tokens, uniform, draft, temperature, None, *ops.verify(target, tokens, uniform, draft=draft, temperature=temperature))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F32])
+@pytest.mark.parametrize("vocab", [1023, 4097, 20001, 131075])
+@pytest.mark.parametrize("spread", [0.5, 3.0])
+def test_equal_rows_leave_nothing_wherever_they_lie(spread, vocab, dtype):
+    """Where target and draft are the same the next token comes from the target, as where the draft's row is empty (a
+    call without drafts' rows cuts the target's into other chunks, whose sums differ in their last bits):
+    rows off one another's place in a vector of 16 bytes are summed in other groups."""
+    b, g = 60, gen(vocab)
+    target = (torch.randn(b, 2, vocab, generator=g, device="cuda") * spread).to(dtype)
+    tokens = torch.full((b, 1), -1, device="cuda")  # (refused)
+    uniform = torch.rand(b, 2, generator=g, device="cuda")
+    store = torch.zeros(b, vocab + 11, device="cuda", dtype=dtype)
+    want = ops.verify(target, tokens, uniform, draft=torch.full_like(target[:, 1:], -math.inf))
+    for first in (0, 1, 3, 8):
+        draft = store[:, None, first:first + vocab]
+        draft.copy_(target[:, :1])
+        got = ops.verify(target, tokens, uniform, draft=draft)
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+        check(target, tokens, uniform, draft, None, None, *got)
