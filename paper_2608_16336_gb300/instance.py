@@ -265,7 +265,7 @@ class Instance:
     @torch.no_grad()
     def speculate(self, drafts: torch.Tensor, *, draft: torch.Tensor | None = None, uniform: torch.Tensor | None = None, temperature=None):
         """One iteration in which every running request advances by its last
-        token and as many of its drafted ones (int64 [requests, n]; -1 or another number outside the vocabulary: none) as
+        token and as many of its drafted ones (int64 [requests, n]; they end at the first -1 or other number outside the vocabulary) as
         ``instance_ops.verify`` accepts, with the token that follows them.  ``draft``, ``uniform`` and
         ``temperature`` as there (default: certain drafts, draws from PyTorch's generator).  Returns (requests,
         tokens [requests, n + 1], -1 behind each request's; how many, on the host; log-probabilities).
@@ -284,7 +284,9 @@ class Instance:
         target = (_norm(x) @ self.unembed).view(len(ids), new, -1)
         if uniform is None:
             uniform = torch.rand(len(ids), new, device="cuda")
-        tokens, count, logprob = ops.verify(target, drafts.contiguous(), uniform, draft=draft, temperature=temperature)
+        # a request's drafts end at the first that is none: the token in its place is the target's, whatever the draft's row holds
+        drafted = ((drafts >= 0) & (drafts < target.shape[-1])).cumprod(1).sum(1, dtype=torch.int32)
+        tokens, count, logprob = ops.verify(target, drafts.contiguous(), uniform, draft=draft, temperature=temperature, drafted=drafted)
         counts = count.tolist()
         del self.free[len(self.free) - taken:]
         self._give_back([b for b, _ in copies])
