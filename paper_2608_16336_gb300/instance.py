@@ -97,10 +97,12 @@ class Instance:
                             key_up=weight(s.heads, s.rank, s.head_dim, fan=s.rank),
                             value_up=weight(s.heads, s.rank, s.value_dim, fan=s.rank),
                             out=weight(s.heads * s.value_dim, s.hidden, fan=s.heads * s.value_dim)) for _ in range(s.layers)]
-        self.cache = torch.zeros(s.layers, blocks, block_tokens, s.rank + s.key_dim, dtype=s.dtype, device="cuda")
-        if quantized:
-            self.cache = self.cache.to(ops.EIGHT)
+        size = s.layers, blocks, block_tokens, s.rank + s.key_dim
+        if quantized:  # (bytes of 0 are zeros)
+            self.cache = torch.zeros(size, dtype=torch.uint8, device="cuda").view(ops.EIGHT)
             self.scales = torch.ones(s.layers, blocks, 2, device="cuda")
+        else:
+            self.cache = torch.zeros(size, dtype=s.dtype, device="cuda")
         self.unembed = weight(s.hidden, s.vocab, fan=s.hidden)
 
     # -- the cache
