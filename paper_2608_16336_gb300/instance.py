@@ -138,6 +138,8 @@ class Instance:
         """``blocks`` with those that a request is about to write (from its
         token ``first`` on) and others hold too replaced by free ones, how many free
         ones are taken with these, and the pairs to be copied.  Changes nothing."""
+        if not self.shared:
+            return blocks, taken, []
         copies, blocks = [], [list(b) for b in blocks]
         left = dict(self.shared)
         for b, n in zip(blocks, first):
@@ -246,11 +248,12 @@ class Instance:
         blocks, taken, copies = self._own(blocks, [self.running[r].length for r in decode] + [0] * len(prompts), taken)
 
         nd = len(decode)
-        x = self.embed[torch.cat([self.running[r].token for r in decode] + prompts)]
+        where = self._where(blocks, lengths, nd, 1, prompts)
+        last = list(range(nd)) + (np.cumsum([len(p) for p in prompts], dtype=np.int64) + (nd - 1)).tolist()
+        last = torch.tensor(last, dtype=torch.int64, device="cuda")
         self._copy(copies)
-        x = self._forward(x, blocks, lengths, nd, 1, prompts)
-        offsets = np.cumsum([0] + [len(p) for p in prompts])
-        last = torch.tensor(list(range(nd)) + [nd + int(o) - 1 for o in offsets[1:]], dtype=torch.int64, device="cuda")
+        x = self.embed[torch.cat([self.running[r].token for r in decode] + prompts)]
+        x = self._forward(x, where, nd, 1, prompts)
         logits = _norm(x[last]) @ self.unembed
         if uniform is None:
             uniform = torch.rand(len(logits), device="cuda")
@@ -280,9 +283,10 @@ class Instance:
         lengths = [n + new for n in held]
         blocks, taken = self._plan([self.running[r].blocks for r in ids], lengths)
         blocks, taken, copies = self._own(blocks, held, taken)
-        x = self.embed[torch.cat((torch.stack([self.running[r].token for r in ids]), drafts.clamp(0, len(self.embed) - 1)), 1).flatten()]
+        where = self._where(blocks, lengths, len(ids), new, [])
         self._copy(copies)
-        x = self._forward(x, blocks, lengths, len(ids), new, [])
+        x = self.embed[torch.cat((torch.stack([self.running[r].token for r in ids]), drafts.clamp(0, len(self.embed) - 1)), 1).flatten()]
+        x = self._forward(x, where, len(ids), new, [])
         target = (_norm(x) @ self.unembed).view(len(ids), new, -1)
         if uniform is None:
             uniform = torch.rand(len(ids), new, device="cuda")
@@ -297,28 +301,26 @@ class Instance:
             self.rewind(r, n + counts[i])
         return ids, tokens, counts, logprob
 
-    def _forward(self, x, blocks, lengths, nd, new, prompts):
-        """The layers over ``nd`` requests' last ``new`` tokens each, then the
-        prompts; ``lengths`` counts every request's tokens with them."""
-        s, t, n = self.shape, self.block_tokens, x.shape[0]
-        # what the kernels read: positions, slots, the running requests' tables, the prompts' offsets
-        positions, slots = [], []
-        for b, k, count in zip(blocks, lengths, [new] * nd + [len(p) for p in prompts]):
-            at = np.arange(k - count, k)
-            positions += at.tolist()
-            slots += (np.asarray(b)[at // t] * t + at % t).tolist()
-        put = lambda v, dtype: torch.tensor(v, dtype=dtype, device="cuda")
-        positions, slots = put(positions, torch.int32), put(slots, torch.int64)
-        every = put(lengths, torch.int32)
+    def _where(self, blocks, lengths, nd, new, prompts):
+        """What the kernels read of ``nd`` requests' last ``new`` tokens each, then
+        the prompts, ``lengths`` counting every request's tokens with them: positions, slots, lengths, the running requests' table (and the
+        prompts', to an 8-bit cache), every request's first row, the prompts' first rows and the longest.
+        (A copy to the device waits for the stream: all of them come before the first kernel.)"""
         quantized = self.scales is not None
+        put = lambda v, dtype: torch.tensor(v, dtype=dtype, device="cuda")
+        positions, slots = _places(blocks, lengths, nd, new, self.block_tokens)
         named = blocks if quantized else blocks[:nd]
         widest = max((len(b) for b in named), default=0)
         table = put([b + [0] * (widest - len(b)) for b in named], torch.int32).reshape(len(named), widest)
         offsets = np.cumsum([0] + [len(p) for p in prompts])
-        longest = max((len(p) for p in prompts), default=0)
-        starts = put(offsets.tolist(), torch.int32)
-        rows = nd * new
-        all_starts = put([new * i for i in range(nd)] + (rows + offsets).tolist(), torch.int32)
+        rows = [new * i for i in range(nd)] + (nd * new + offsets).tolist()
+        return (put(positions, torch.int32), None if quantized else put(slots, torch.int64), put(lengths if quantized else lengths[:nd], torch.int32), table,
+                put(rows, torch.int32) if quantized else None, put(offsets.tolist(), torch.int32), max((len(p) for p in prompts), default=0))
+
+    def _forward(self, x, where, nd, new, prompts):
+        """The layers over ``nd`` requests' last ``new`` tokens each, then the prompts."""
+        s, n, rows, quantized = self.shape, x.shape[0], nd * new, self.scales is not None
+        positions, slots, every, table, all_starts, starts, longest = where
         for i, (layer, cache) in enumerate(zip(self.layers, self.cache)):
             h = _norm(x)
             q = (h @ layer["q"]).view(n, s.heads, s.head_dim + s.key_dim)
@@ -337,7 +339,7 @@ class Instance:
                 if quantized:
                     ops.quantized_decode(inner, cache, self.scales[i], table[:nd], every[:nd], scale=self.scale, out=got)
                 else:
-                    ops.latent_decode(inner, cache, table, every[:nd], scale=self.scale, out=got)
+                    ops.latent_decode(inner, cache, table, every, scale=self.scale, out=got)
                 out[:rows] = torch.matmul(got.flatten(0, 1).transpose(0, 1), layer["value_up"]).transpose(0, 1)
             if prompts:  # expanded: every head has keys and values of its own
                 keys = torch.matmul(latent[rows:], layer["key_up"]).transpose(0, 1)
@@ -348,6 +350,20 @@ class Instance:
             if self.feed_forward is not None:
                 x = self.feed_forward(x)
         return x
+
+
+def _places(blocks, lengths, nd, new, t):
+    """Positions and slots of ``nd`` requests' last ``new`` tokens each, then of whole prompts, in blocks of ``t`` tokens."""
+    positions, slots = [], []
+    for b, k in zip(blocks[:nd], lengths):  # (a long request's blocks are not gone through for a token)
+        for p in range(k - new, k):
+            positions.append(p)
+            slots.append(b[p // t] * t + p % t)
+    for b, k in zip(blocks[nd:], lengths[nd:]):
+        at = np.arange(k)
+        positions += at.tolist()
+        slots += (np.asarray(b)[at // t] * t + at % t).tolist()
+    return positions, slots
 
 
 def measure(node: Instance, *, prefill_tokens=(0, 256, 1024, 4096), decodes=(0, 8, 32, 63), context: int = 512, repeats: int = 3):
