@@ -201,10 +201,12 @@ __global__ void __launch_bounds__(kThreads) k_quantized_append(const __grid_cons
         } else if (HOW == kOnes) {
             for (int i = lane; i < a.rank; i += 32) row[i] = (uint8_t)pack_e4m3(stored(elem<T>::to(x[i]), by0), 0.f);
         }
-        if (WIDE && kept) {
-            for (int i = 8 * lane; i < a.rot_dim; i += 256) {  // (the warp's own)
-                const float *f = keys + (r - w.r0) * a.rot_dim + i;
-                *(uint2 *)(row + a.rank + i) = make_uint2(four_of(f, by1), four_of(f + 4, by1));
+        if (kept) {  // (the warp's own)
+            const float *f = keys + (r - w.r0) * a.rot_dim;
+            if (WIDE) {
+                for (int i = 8 * lane; i < a.rot_dim; i += 256) *(uint2 *)(row + a.rank + i) = make_uint2(four_of(f + i, by1), four_of(f + i + 4, by1));
+            } else {
+                for (int i = lane; i < a.rot_dim; i += 32) row[a.rank + i] = (uint8_t)pack_e4m3(stored(f[i], by1), 0.f);
             }
         } else {
             for (int i = lane; i < half; i += 32) {
