@@ -56,6 +56,21 @@ def test_blocks_are_gone_through_only_where_some_are_shared():
     assert node._own(blocks, [9, 8], 3)[1:] == (3, []) and Counted.looks == 0
 
 
+def test_refused_calls_leave_the_count_of_shared_blocks(monkeypatch):
+    monkeypatch.setattr(instance.Instance, "_copy", lambda self, pairs, other=None: None)
+    node, other = bookkeeping(7, 4, [9, 8]), bookkeeping(2, 4, [3])
+    node.fork(1), node.fork(0)
+    kept = dict(node.shared)
+    assert kept == {b: 1 for b in node.running[1].blocks + node.running[0].blocks[:2]}
+    drafts = torch.zeros(4, 20, dtype=torch.int64)
+    for call, error in ((lambda: node.fork(0, 2), RuntimeError), (lambda: node.fork(1, 9), ValueError), (lambda: node.migrate(1, other), RuntimeError),
+                        (lambda: node.rewind(0, 10), ValueError), (lambda: node.iterate([torch.zeros(40, dtype=torch.int64)]), RuntimeError),
+                        (lambda: node.speculate(drafts), RuntimeError), (lambda: node.speculate(drafts[:3]), ValueError)):
+        with pytest.raises(error):
+            call()
+        assert node.shared == kept and not other.shared
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("quantized", [False, True])
 def test_no_copy_to_the_device_waits_for_the_layers(quantized, monkeypatch):
