@@ -241,7 +241,7 @@ int sim_op_sample(const sim_op_sample_t *args, void *cuda_stream);
  * lengths[b] - n .. lengths[b] - 1 (lengths counts cached tokens, the new ones
  * included; a token's index is its rotary position).  Token p is row p % T of block table[b][p / T]:
  * [latent, rotated key (as above, with amplitude)], divided by the block's scales and
- * rounded to the nearest e4m3 (ties to even).  Nothing is rounded before that.
+ * rounded to the nearest e4m3 (ties to even).  Nothing is rounded before that (but the quotient to 32 bits, by a scale that is no power of two).
  * A block's scales come from what is written.  need = the smallest power of
  * two in [2^-60, 2^60] with max |x| <= 448 * need over the rows of this call in
  * the block.  Where row 0 is among them the block begins anew and its scale is need;
@@ -333,7 +333,9 @@ size_t sim_op_quantized_decode_workspace(int32_t requests, int32_t new_tokens, i
  * NaN logits count as -infinity; with +infinite logits the probability is shared
  * by these.  In a row without a logit above -infinity every probability is 0: a drafted token is refused there, a draw
  * gives -1 and -infinity.  A drafted token outside [0, vocab) has probability 0
- * under both.  Weights exp((l - max) / t) are in 32 bits (one below 2^-126 is 0), sums over the vocabulary in 64. */
+ * under both.  Weights exp((l - max) / t) are in 32 bits, good to 2^-22 (one below 2^-126 is 0).  A row's are summed in 32 bits by threads and
+ * warps of them, in pairs of 32-bit numbers above, and the total is rounded to 32: a probability is good to 6e-7 of itself in vocabularies up to
+ * 2^17, to 1e-6 up to 2^20.  The draw goes by whole numbers of 2^-50, into which the probabilities of 16 bytes of logits are cut together. */
 typedef struct {
     const void *target;         /* [requests][drafts + 1][vocab] */
     const void *draft;          /* [requests][drafts][vocab], the target's type, or NULL */

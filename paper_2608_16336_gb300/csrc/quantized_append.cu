@@ -83,7 +83,8 @@ template <typename T> __device__ __forceinline__ void eight(const T *x, float *f
 
 // HOW: an element at a time; rows that are made of whole vectors of 8 elements; the same where a
 // warp's rows fit its registers (16-bit rows of up to 512 elements, blocks of up to 16), so that all loads are
-// asked for at once and nothing is read again: prompts of 20,000 tokens (32 MB) 13.2 us, else 17.6.
+// asked for at once and nothing is read again: prompts of 20,000 float16 tokens (32 MB) 13.2 us, else 17.6 (bfloat16 ones, with
+// 96 registers instead of 72, in blocks of 12 20.4).
 enum { kOnes, kWide, kHeld };
 constexpr int kHeldRows = 4, kHeldRank = 512;
 template <typename T, int HOW>

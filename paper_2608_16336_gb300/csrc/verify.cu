@@ -14,10 +14,10 @@ namespace cg = cooperative_groups;
 // accepted, goes once more over the one row (or the two) that the next token is drawn from, and the
 // warp whose stretch holds the point looks for it.
 // 64 requests, 4 rows of 131,075 bfloat16 logits and 3 of the draft (117 MB) take 49 us: the rows 25, bound by instructions (11 a
-// logit; 62 registers and two blocks a multiprocessor 33), the draw 21, bound by waiting for its loads.
+// logit; 62 registers and two blocks a multiprocessor 33; three leave 40 registers, and the bfloat16 kernel has 72 bytes on its stack besides), the draw 21, bound by waiting for its loads.
 //
-// Nothing is in 64-bit floating point, which runs at a sixtieth of the rate here (a division by every thread took
-// 58 of 165 us).  Sums of single threads and warps are 32-bit floats, whose errors are independent and average out; sums
+// Nothing is in 64-bit floating point, which runs at a sixtieth of the rate here (with it these two kernels took 165 us for that, 58 of
+// them a division by every thread).  Sums of single threads and warps are 32-bit floats, whose errors are independent and average out; sums
 // of those are pairs of floats, and the masses that the draw goes by are whole numbers of 2^-50, which add up the same in any order.
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBatch = 4;            // vectors that a thread has on their way
@@ -29,7 +29,7 @@ typedef unsigned long long u64;
 struct Rate {
     float hi, lo;
     bool greedy;
-    // (In 32 bits: a 64-bit division by every thread took 58 us of 64 requests' 90.)
+    // (A 32-bit division and its rest.)
     __device__ __forceinline__ explicit Rate(float t) {
         greedy = !(t > 0.f);
         const float q = 1.44269502f / (greedy ? 1.f : t), rest = fmaf(-q, t, 1.44269502f) + 1.92596303e-8f, more = rest / t;

@@ -272,7 +272,8 @@ class Instance:
         """One iteration in which every running request advances by its last
         token and as many of its drafted ones (int64 [requests, n]; they end at the first -1 or other number outside the vocabulary) as
         ``instance_ops.verify`` accepts, with the token that follows them.  ``draft``, ``uniform`` and
-        ``temperature`` as there (default: certain drafts, draws from PyTorch's generator).  Returns (requests,
+        ``temperature`` as there (default: certain drafts, draws from PyTorch's generator).  Tokens follow the target's whole
+        distribution: there is no top-k, top-p or min-p as in ``iterate``.  Returns (requests,
         tokens [requests, n + 1], -1 behind each request's; how many, on the host; log-probabilities).
         A call that raises leaves the batch and the free blocks as they were."""
         ids = list(self.running)

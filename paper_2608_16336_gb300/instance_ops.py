@@ -464,7 +464,9 @@ def quantized_append(latent, key, frequencies, offsets, table, lengths, cache, s
 def quantized_decode(q, cache, scales, table, lengths, *, scale, out=None, lse=None):
     """``latent_decode`` over an 8-bit cache as ``quantized_append`` fills it:
     ``cache`` float8_e4m3fn [blocks, block_tokens, width], ``scales`` float32
-    [blocks, 2].  Returns (out [requests, new, heads, rank] in q's type, lse float32)."""
+    [blocks, 2].  ``rank``, the elements of a row's latent part (with the first scale; the
+    values), is ``out``'s last dimension, or width - 64 without ``out``: a cache with another key part, or
+    none, needs ``out``.  Returns (out [requests, new, heads, rank] in q's type, lse float32)."""
     if q.dim() != 4 or table.dim() != 2:
         raise ValueError("q must be [requests, new, heads, width], table [requests, n]")
     b, new, heads, width = q.shape
